@@ -1,5 +1,6 @@
 /*
- * atomo.h -- C ABI of the B200 (sm_100a) ATOMO gradient encode / decode library.
+ * atomo.h -- C ABI of the B200 (sm_100a) ATOMO gradient encode / decode library, with the operators that
+ * stand on either side of the exchange in a training step (embedding, layer norm; gradient norm, AdamW).
  *
  * ATOMO ("atomic sparsification") writes a gradient as g = sum_i lambda_i a_i over unit-norm
  * atoms a_i, keeps atom i with probability p_i and rescales it by 1/p_i, so that the sparse
@@ -250,6 +251,96 @@ enum { ATOMO_STATIC_MAX_LAYERS = 64, ATOMO_STATIC_MAX_TILES = 8192 };
 int atomo_decode_spectral_static(int device, const void* payload /*DEVICE*/, const int64_t* rows,
                                  const int64_t* cols, float* const* out /*HOST array of DEVICE ptrs*/,
                                  int32_t n_layers, void* stream);
+
+/* ==============================================================================================
+ * Operators on either side of the exchange (the paper has no counterpart).  Before it: the two layers of a language model
+ * whose weight gradients are sums over the tokens, embedding and layer norm; their gradients come in fp32, with a leading
+ * dimension and summed in a fixed order, as the encode calls take them.  Behind it: the global norm of the decoded gradients
+ * and the AdamW step over all parameters.
+ *   - Values are fp32, bf16 or fp16 (atomo_type); arithmetic, sums and statistics are in fp32 or fp64, and a result is rounded to
+ *     its type once, to the nearest value.  Pointers need the alignment of their type alone; 16-byte aligned
+ *     rows and tensors are moved faster.
+ *   - No call allocates or waits on the host: what a call needs beside its operands is a workspace of the caller
+ *     (atomo_*_workspace_bytes, host only; contents need not be kept), so that calls on several streams, and CUDA graphs that hold
+ *     them, share nothing.  A captured call keeps the host values it was captured with (learning rate, step, seed).
+ *   - The same call gives the same bits each time.
+ *   - The current device of the calling thread is left as it was.                              */
+typedef enum { ATOMO_TYPE_F32 = 0, ATOMO_TYPE_BF16 = 1, ATOMO_TYPE_F16 = 2 } atomo_type;
+typedef struct { const void* data; /* DEVICE */ int64_t n; int32_t type; /* atomo_type */ int32_t reserved; } atomo_tensor;
+
+/* --- gradient norm -----------------------------------------------------------------------------
+ * out[0] = sqrt(sum of the squares of all elements of all tensors), out[1] = min(1, max_norm / (out[0] + 1e-6)): the norm and the
+ * factor that clips the gradients to it.  max_norm > 0; INFINITY asks for the norm alone (factor 1).  The sum neither
+ * overflows nor underflows: out[0] is the norm rounded to fp32.  Where an element is NaN or Inf the norm is not finite and
+ * the factor is NaN.  Tensors may be empty; at most 2^20 of them.  workspace: atomo_grad_norm_workspace_bytes().               */
+int64_t atomo_grad_norm_workspace_bytes(void);
+int atomo_grad_norm(atomo_ctx* ctx, const atomo_tensor* grads /*HOST array*/, int32_t n_tensors, double max_norm,
+                    float* out /*DEVICE, 2 floats*/, void* workspace /*DEVICE*/, int64_t workspace_bytes, void* stream);
+
+/* --- AdamW over a list of parameters -------------------------------------------------------------
+ *   m = beta1 m + (1 - beta1) c g,  v = beta2 v + (1 - beta2) (c g)^2,
+ *   p = p - lr weight_decay p - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * with c = scale[1] (DEVICE, as atomo_grad_norm leaves it; NULL: c = 1).  A c that is not finite leaves every parameter and state as
+ * it is.  grads[i] belongs to tensors[i] and has n elements of grad_type.  With `master` the fp32 copy is what is
+ * updated, and param receives it rounded; without it param is read and written in its own type.
+ *   State in 32 bits: exp_avg and exp_avg_sq are fp32[n], the scales NULL.
+ *   State in 8 bits: exp_avg and exp_avg_sq are OCP e4m3 numbers, one byte each; exp_avg_scale and exp_avg_sq_scale hold one byte
+ * for each ATOMO_STATE_BLOCK elements (the last block may be shorter): a code's value is e4m3(code) * 2^(byte - 127).  All zero bytes are a
+ * state of zero.  The new state is rounded up or down at random in proportion (so that it stays unbiased: rounded to the nearest, an
+ * average would stand still where a step changes it by less than half a unit), by the Philox words of the conventions
+ * above with key = seed and counter = (i>>2 low, 2^31 | i>>2 high, tensor, step & 0x7fffffff), which no encode uses: element i takes the low 16 bits of
+ * word i&3 for the first moment, the high ones for the second.  A second moment above zero is not rounded to zero.  A state that is not finite becomes NaN.
+ * The parameters in `tensors` and their states do not overlap; a parameter may be empty.  Every n < 2^34 with 8-bit states.      */
+enum { ATOMO_STATE_BLOCK = 32 };
+typedef struct {
+  void* param;                                  /* DEVICE, type                                 */
+  void *exp_avg, *exp_avg_sq;                   /* DEVICE                                       */
+  uint8_t *exp_avg_scale, *exp_avg_sq_scale;    /* DEVICE, 8-bit states only                    */
+  float* master;                                /* DEVICE or NULL                               */
+  int64_t n;
+  float weight_decay;
+  int32_t type;                                 /* atomo_type of param                          */
+} atomo_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps;                 /* lr, eps >= 0; 0 <= beta < 1                  */
+  int64_t step;                                 /* 1 for the first step                         */
+  uint64_t seed;                                /* 8-bit states                                 */
+  const float* scale;                           /* DEVICE, 2 floats, or NULL                    */
+  int32_t state_bits, grad_type;                /* 32 or 8; atomo_type                          */
+} atomo_adamw_args;
+int atomo_adamw(atomo_ctx* ctx, const atomo_adamw_tensor* tensors /*HOST array*/, const void* const* grads /*HOST array of DEVICE ptrs*/,
+                int32_t n_tensors, const atomo_adamw_args* args /*HOST*/, void* stream);
+
+/* --- embedding -----------------------------------------------------------------------------------
+ * out[t] = scale * table[ids[t]]: table is rows x cols of `type` with leading dimension ld, out n_ids x cols of the same type with
+ * leading dimension ld_out; ids are 4 or 8 bytes wide (id_bytes).  An id outside [0, rows) gives a row of zeros and, where status (DEVICE,
+ * one int32, set to 0 by the caller) is not NULL, ATOMO_ERR_INVALID_ARG in it.
+ * Backward: out[v] = scale * sum of grad[t] over the tokens t with ids[t] = v, in the order of the tokens; out is fp32, every
+ * element of its rows x cols is written (accumulate != 0: added to what is there).  grad is n_ids x cols of `type`, leading dimension ld.  Tokens whose id
+ * is padding_idx (-1: none) or lies outside [0, rows) are left out; the latter raise status.
+ * 0 <= n_ids < 2^31, rows < 2^31, cols <= 2^24.  workspace: atomo_embedding_workspace_bytes (-1 on bad arguments).               */
+int atomo_embedding(atomo_ctx* ctx, const void* table /*DEVICE*/, int32_t type, int64_t rows, int64_t cols, int64_t ld,
+                    const void* ids /*DEVICE*/, int32_t id_bytes, int64_t n_ids, double scale, void* out /*DEVICE*/, int64_t ld_out,
+                    int32_t* status /*DEVICE or NULL*/, void* stream);
+int64_t atomo_embedding_workspace_bytes(int64_t n_ids, int64_t rows, int64_t cols);
+int atomo_embedding_backward(atomo_ctx* ctx, const void* ids /*DEVICE*/, int32_t id_bytes, int64_t n_ids, const void* grad /*DEVICE*/, int32_t type,
+                             int64_t ld, int64_t rows, int64_t cols, double scale, int64_t padding_idx, float* out /*DEVICE*/, int64_t ld_out,
+                             int32_t accumulate, int32_t* status /*DEVICE or NULL*/, void* workspace /*DEVICE*/, int64_t workspace_bytes, void* stream);
+
+/* --- layer norm ------------------------------------------------------------------------------------
+ * Over the cols values of each row: y = (x - mean) rstd weight + bias, rstd = 1 / sqrt(variance + eps).  x and y are rows x cols of `type` with
+ * leading dimensions; weight and bias (either may be NULL: ones, zeros) cols values of weight_type; mean and rstd fp32[rows] are kept for the
+ * backward pass, which gives dx (rows x cols of `type`) and, where not NULL, the sums over the rows dweight and dbias (fp32[cols]).
+ * y may be x, and dx may be dy or x (same leading dimension).  0 <= rows < 2^31, 1 <= cols <= 2^24, eps >= 0.
+ * workspace: atomo_layer_norm_workspace_bytes (-1 on bad arguments).                                                               */
+int atomo_layer_norm(atomo_ctx* ctx, const void* x /*DEVICE*/, int32_t type, int64_t rows, int64_t cols, int64_t ld, const void* weight /*DEVICE or NULL*/,
+                     const void* bias /*DEVICE or NULL*/, int32_t weight_type, double eps, void* y /*DEVICE*/, int64_t ld_y, float* mean /*DEVICE*/,
+                     float* rstd /*DEVICE*/, void* stream);
+int64_t atomo_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+int atomo_layer_norm_backward(atomo_ctx* ctx, const void* dy /*DEVICE*/, int64_t ld_dy, const void* x /*DEVICE*/, int64_t ld_x, int32_t type, int64_t rows,
+                              int64_t cols, const void* weight /*DEVICE or NULL*/, int32_t weight_type, const float* mean /*DEVICE*/, const float* rstd /*DEVICE*/,
+                              void* dx /*DEVICE*/, int64_t ld_dx, float* dweight /*DEVICE or NULL*/, float* dbias /*DEVICE or NULL*/,
+                              void* workspace /*DEVICE*/, int64_t workspace_bytes, void* stream);
 
 /* --- status / introspection -----------------------------------------------------------------
  * Copies the payload header and the n_layers layer headers to HOST memory (synchronises

@@ -36,7 +36,11 @@ EXPORTS = [
     "atomo_set_tridiag_ctas", "atomo_limit_tridiag_route", "atomo_limit_workspace", "atomo_measure_fma_peak", "atomo_encode_spectral_from_svd", "atomo_get_table_uploads",
     "atomo_set_entrywise_launch",
     "atomo_get_entrywise_list_chunks",
+    "atomo_grad_norm_workspace_bytes", "atomo_grad_norm", "atomo_adamw", "atomo_embedding", "atomo_embedding_workspace_bytes",
+    "atomo_embedding_backward", "atomo_layer_norm", "atomo_layer_norm_workspace_bytes", "atomo_layer_norm_backward",
 ]
+TYPE_CODES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # atomo_type
+STATE_BLOCK = 32                     # elements of an 8-bit optimiser state that share a power of two
 
 
 class AtomoError(RuntimeError):
@@ -57,6 +61,21 @@ class _Vec(ctypes.Structure):
 class _Debug(ctypes.Structure):
     _fields_ = [("sigma", ctypes.c_void_p), ("prob", ctypes.c_void_p), ("mask_words", ctypes.c_void_p),
                 ("short_vecs", ctypes.c_void_p)]
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class _AdamWTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p), ("exp_avg_scale", ctypes.c_void_p),
+                ("exp_avg_sq_scale", ctypes.c_void_p), ("master", ctypes.c_void_p), ("n", ctypes.c_int64), ("weight_decay", ctypes.c_float),
+                ("type", ctypes.c_int32)]
+
+
+class _AdamWArgs(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double), ("step", ctypes.c_int64),
+                ("seed", ctypes.c_uint64), ("scale", ctypes.c_void_p), ("state_bits", ctypes.c_int32), ("grad_type", ctypes.c_int32)]
 
 
 class PayloadHeader(ctypes.Structure):
@@ -129,6 +148,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.atomo_measure_fma_peak.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_double)]
     lib.atomo_decode_spectral_static.argtypes = [ctypes.c_int, vp, ctypes.POINTER(i64), ctypes.POINTER(i64),
                                                  ctypes.POINTER(vp), i32, vp]
+    lib.atomo_grad_norm_workspace_bytes.argtypes = []
+    lib.atomo_grad_norm_workspace_bytes.restype = i64
+    lib.atomo_grad_norm.argtypes = [vp, ctypes.POINTER(_Tensor), i32, dbl, vp, vp, i64, vp]
+    lib.atomo_adamw.argtypes = [vp, ctypes.POINTER(_AdamWTensor), ctypes.POINTER(vp), i32, ctypes.POINTER(_AdamWArgs), vp]
+    lib.atomo_embedding.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, i64, dbl, vp, i64, vp, vp]
+    lib.atomo_embedding_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.atomo_embedding_workspace_bytes.restype = i64
+    lib.atomo_embedding_backward.argtypes = [vp, vp, i32, i64, vp, i32, i64, i64, i64, dbl, i64, vp, i64, i32, vp, vp, i64, vp]
+    lib.atomo_layer_norm.argtypes = [vp, vp, i32, i64, i64, i64, vp, vp, i32, dbl, vp, i64, vp, vp, vp]
+    lib.atomo_layer_norm_workspace_bytes.argtypes = [i64, i64]
+    lib.atomo_layer_norm_workspace_bytes.restype = i64
+    lib.atomo_layer_norm_backward.argtypes = [vp, vp, i64, vp, i64, i32, i64, i64, vp, i32, vp, vp, vp, i64, vp, vp, vp, i64, vp]
     if path == LIB_PATH:
         _lib = lib
     return lib
@@ -179,6 +210,11 @@ def measure_fma_peak(device: int = 0, fp64: bool = False) -> float:
     if rc != 0:
         raise AtomoError(rc, "atomo_measure_fma_peak")
     return float(out.value)
+
+
+@functools.lru_cache(maxsize=1)
+def _grad_norm_bytes() -> int:
+    return int(load_library().atomo_grad_norm_workspace_bytes())
 
 
 def default_k_cap(s: float, n_atoms: int) -> int:
@@ -307,6 +343,96 @@ def atomo_decode_spectral_static(payload: "Payload", out: Sequence[torch.Tensor]
     return list(out)
 
 
+def _rows(t: torch.Tensor, cols: int, what: str):
+    """(rows, leading dimension) of a tensor seen as a matrix over its last dimension; its rows must lie at one distance."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 0 or shape[-1] != cols or (cols > 1 and stride[-1] != 1):
+        raise ValueError(f"{what}: a tensor with {cols} values in its last dimension, of unit stride, is required")
+    if t.is_contiguous():
+        return t.numel() // cols, cols
+    if len(shape) == 1:
+        return 1, cols
+    rows, ld = shape[-2], stride[-2] if shape[-2] > 1 else cols
+    for n, s in zip(reversed(shape[:-2]), reversed(stride[:-2])):
+        if rows > 1 and n > 1 and s != rows * ld:
+            raise ValueError(f"{what}: its rows do not lie at one distance")
+        if n > 1 and rows == 1:
+            ld = s
+        rows *= n
+    if rows > 1 and ld < cols:
+        raise ValueError(f"{what}: its rows overlap")
+    return rows, max(ld, cols)
+
+
+class AdamWState:
+    """Parameters and their optimiser states as atomo_adamw takes them.
+
+    params: contiguous CUDA tensors of one device, fp32, bf16 or fp16.  State in 32 bits: exp_avg and exp_avg_sq are fp32 tensors of as many
+    elements.  State in 8 bits: float8_e4m3fn tensors of as many elements, with exp_avg_scale and exp_avg_sq_scale of one
+    float8_e8m0fnu number for each 32 elements.  master: fp32 copies that are updated instead of the parameters, which then receive them
+    rounded (None, or a list in which single entries may be None).  weight_decay: one number, or one per parameter.
+    The object keeps the tensors and describes their memory once: they are updated in place and must not be given
+    other memory.  `AdamWState.zeros(params, bits=...)` makes the states of a new run."""
+
+    def __init__(self, params: Sequence[torch.Tensor], exp_avg: Sequence[torch.Tensor], exp_avg_sq: Sequence[torch.Tensor],
+                 exp_avg_scale: Optional[Sequence[torch.Tensor]] = None, exp_avg_sq_scale: Optional[Sequence[torch.Tensor]] = None,
+                 master: Optional[Sequence[Optional[torch.Tensor]]] = None, weight_decay=0.01):
+        n = len(params)
+        if n == 0:
+            raise ValueError("at least one parameter is required")
+        if (exp_avg_scale is None) != (exp_avg_sq_scale is None):
+            raise ValueError("both states have scales, or neither")
+        self.bits = 32 if exp_avg_scale is None else 8
+        self.params, self.exp_avg, self.exp_avg_sq = list(params), list(exp_avg), list(exp_avg_sq)
+        self.exp_avg_scale = [None] * n if exp_avg_scale is None else list(exp_avg_scale)
+        self.exp_avg_sq_scale = [None] * n if exp_avg_sq_scale is None else list(exp_avg_sq_scale)
+        self.master = [None] * n if master is None else list(master)
+        self.weight_decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        lists = (self.exp_avg, self.exp_avg_sq, self.exp_avg_scale, self.exp_avg_sq_scale, self.master, self.weight_decay)
+        if any(len(x) != n for x in lists):
+            raise ValueError("one state, scale, master copy and weight decay per parameter is required")
+        if any(not (w >= 0.0 and np.isfinite(w)) for w in self.weight_decay):
+            raise ValueError("weight decays are finite and not negative")
+        state = torch.float32 if self.bits == 32 else torch.float8_e4m3fn
+        dev, desc, ranges = self.params[0].device, [], []
+        self.lengths = []
+        for i, (p, m, v, ms, vs, w) in enumerate(zip(self.params, *lists[:5])):
+            size = p.numel()
+            blocks = -(-size // STATE_BLOCK)
+            parts = [("parameter", p, size, None), ("exp_avg", m, size, state), ("exp_avg_sq", v, size, state)]
+            if self.bits == 8:
+                parts += [("exp_avg_scale", ms, blocks, torch.float8_e8m0fnu), ("exp_avg_sq_scale", vs, blocks, torch.float8_e8m0fnu)]
+            if w is not None:
+                parts.append(("master copy", w, size, torch.float32))
+            for name, t, count, kind in parts:
+                if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == dev and t.is_contiguous() and t.numel() == count
+                        and (t.dtype in TYPE_CODES if kind is None else t.dtype == kind)):
+                    raise ValueError(f"{name} {i}: a contiguous CUDA tensor on {dev} with {count} elements of "
+                                     f"{'fp32, bf16 or fp16' if kind is None else kind} is required")
+                if count:
+                    ranges.append((t.data_ptr(), t.data_ptr() + count * t.element_size()))
+            desc.append((p.data_ptr(), m.data_ptr(), v.data_ptr(), None if ms is None else ms.data_ptr(), None if vs is None else vs.data_ptr(),
+                         None if w is None else w.data_ptr(), size, self.weight_decay[i], TYPE_CODES[p.dtype]))
+            self.lengths.append(size)
+        ranges.sort()
+        if any(a[1] > b[0] for a, b in zip(ranges, ranges[1:])):
+            raise ValueError("parameters and states must not overlap")
+        self.device = dev
+        self._desc = (_AdamWTensor * n)(*desc)
+
+    @classmethod
+    def zeros(cls, params: Sequence[torch.Tensor], bits: int = 32, master: bool = False, weight_decay=0.01) -> "AdamWState":
+        """The state of a run that has made no step.  master: keep fp32 copies of the parameters that are not fp32."""
+        if bits not in (8, 32):
+            raise ValueError("states have 8 or 32 bits")
+        kind = torch.float32 if bits == 32 else torch.float8_e4m3fn
+        moments = [[torch.zeros(p.numel(), dtype=torch.uint8 if bits == 8 else kind, device=p.device).view(kind) for p in params] for _ in range(2)]
+        scales = [[torch.zeros(-(-p.numel() // STATE_BLOCK), dtype=torch.uint8, device=p.device).view(torch.float8_e8m0fnu) for p in params]
+                  for _ in range(2)] if bits == 8 else [None, None]
+        copies = [p.detach().float().clone() if p.dtype != torch.float32 else None for p in params] if master else None
+        return cls(params, moments[0], moments[1], scales[0], scales[1], copies, weight_decay)
+
+
 class Atomo:
     """One library context bound to a CUDA device."""
 
@@ -315,6 +441,7 @@ class Atomo:
             raise RuntimeError("atomo: no CUDA device available (the library has no CPU fallback)")
         self.lib = load_library()
         self.device = int(device)
+        self._torch_device = torch.device("cuda", self.device)
         torch.cuda.init()
         h = ctypes.c_void_p()
         rc = self.lib.atomo_create(ctypes.byref(h), self.device)
@@ -514,6 +641,201 @@ class Atomo:
         out = (ctypes.c_double * n)()
         self._check(self.lib.atomo_lq_budget(self._h, arr, n, float(q), out, self._stream_ptr(stream)), "atomo_lq_budget")
         return [float(x) for x in out]
+
+    # ---- operators on either side of the exchange ---------------------------------------------
+    def _own_stream(self, stream: Optional[torch.cuda.Stream]) -> int:
+        """The stream given, or the current one of the context's device (whatever device is current)."""
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self.device)
+        if stream.device_index != self.device:
+            raise ValueError(f"the stream belongs to device {stream.device_index}, the context to device {self.device}")
+        return stream.cuda_stream
+
+    def _scratch(self, nbytes: int, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+        """A workspace for one call: torch's allocator keeps it from other work of this stream's order, also in a captured graph."""
+        t = torch.empty(nbytes, dtype=torch.uint8, device=self._torch_device)
+        if stream is not None:
+            t.record_stream(stream)
+        return t
+
+    def _operand(self, t, what: str, types=TYPE_CODES) -> torch.Tensor:
+        if not (isinstance(t, torch.Tensor) and t.get_device() == self.device and t.dtype in types):
+            raise ValueError(f"{what}: a CUDA tensor on device {self.device} of type {', '.join(str(x) for x in types)} is required")
+        return t
+
+    def atomo_grad_norm(self, grads: Sequence[torch.Tensor], max_norm: float = float("inf"), out: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """Two fp32 numbers on the device: the 2-norm over all elements of all gradients, and min(1, max_norm / (norm + 1e-6)), the factor
+        that clips them (NaN where the norm is not finite), as atomo_adamw takes them.  Gradients: contiguous fp32, bf16 or fp16."""
+        device, codes = self.device, TYPE_CODES
+        desc = []
+        for g in grads:
+            code = codes.get(g.dtype)
+            if code is None or g.get_device() != device or not g.is_contiguous():
+                raise ValueError(f"gradients must be contiguous fp32, bf16 or fp16 tensors on CUDA device {device}")
+            desc.append((g.data_ptr(), g.numel(), code, 0))
+        n = len(desc)
+        if out is None:
+            out = torch.empty(2, dtype=torch.float32, device=self._torch_device)
+        elif not (out.get_device() == device and out.dtype == torch.float32 and out.numel() == 2 and out.is_contiguous()):
+            raise ValueError(f"out: two fp32 numbers on CUDA device {device} are required")
+        s = self._own_stream(stream)
+        ws = self._scratch(_grad_norm_bytes(), stream)
+        self._check(self.lib.atomo_grad_norm(self._h, (_Tensor * n)(*desc), n, float(max_norm), out.data_ptr(), ws.data_ptr(), ws.numel(), s), "atomo_grad_norm")
+        return out
+
+    def atomo_adamw(self, state: AdamWState, grads: Sequence[torch.Tensor], lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999,
+                    eps: float = 1e-8, seed: int = 0, scale: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+        """One AdamW step (decoupled weight decay) over all parameters of `state`, in place.  grads: one contiguous tensor per parameter, all of
+        one type.  step counts from 1.  scale: what atomo_grad_norm returned; its second number multiplies the gradients, and where it
+        is not finite nothing is updated.  seed: of the stochastic rounding of 8-bit states."""
+        n, device = len(state.lengths), self.device
+        if len(grads) != n:
+            raise ValueError(f"{n} gradients are required")
+        if state.device.index != device:
+            raise ValueError(f"the parameters are on {state.device}, the context on device {device}")
+        kind = grads[0].dtype
+        if kind not in TYPE_CODES:
+            raise ValueError("gradients must be fp32, bf16 or fp16")
+        ptrs = []
+        for g, size in zip(grads, state.lengths):
+            if g.dtype is not kind or g.numel() != size or g.get_device() != device or not g.is_contiguous():
+                raise ValueError(f"gradients must be contiguous tensors of one type on CUDA device {device}, with as many elements as their parameters")
+            ptrs.append(g.data_ptr())
+        if scale is not None and not (scale.get_device() == device and scale.dtype == torch.float32 and scale.numel() == 2 and scale.is_contiguous()):
+            raise ValueError(f"scale: two fp32 numbers on CUDA device {device} are required")
+        args = _AdamWArgs(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, None if scale is None else scale.data_ptr(), state.bits, TYPE_CODES[kind])
+        rc = self.lib.atomo_adamw(self._h, state._desc, (ctypes.c_void_p * n)(*ptrs), n, ctypes.byref(args), self._own_stream(stream))
+        self._check(rc, "atomo_adamw")
+
+    def _status(self, status: Optional[torch.Tensor]):
+        if status is None:
+            return None
+        if not (status.get_device() == self.device and status.dtype == torch.int32 and status.numel() == 1):
+            raise ValueError(f"status: one int32 number on CUDA device {self.device} is required")
+        return status.data_ptr()
+
+    def _ids(self, ids: torch.Tensor) -> int:
+        if not (isinstance(ids, torch.Tensor) and ids.get_device() == self.device and ids.is_contiguous() and ids.dtype in (torch.int32, torch.int64)):
+            raise ValueError(f"ids: a contiguous int32 or int64 tensor on CUDA device {self.device} is required")
+        return 8 if ids.dtype == torch.int64 else 4
+
+    def atomo_embedding(self, table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+                        status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """scale * table[ids], of shape ids.shape + (cols,).  An id outside the table gives a row of zeros and raises `status` (one int32, set to
+        zero by the caller) to ATOMO_ERR_INVALID_ARG."""
+        code = TYPE_CODES[self._operand(table, "table").dtype]
+        if table.dim() != 2:
+            raise ValueError("table: a matrix is required")
+        cols = table.shape[1]
+        rows, ld = _rows(table, cols, "table")
+        width = self._ids(ids)
+        n = ids.numel()
+        if out is None:
+            out = torch.empty((*ids.shape, cols), dtype=table.dtype, device=table.device)
+            ld_out = cols
+        else:
+            n_out, ld_out = _rows(self._operand(out, "out", (table.dtype,)), cols, "out")
+            if n_out != n:
+                raise ValueError(f"out: {n} rows are required")
+        rc = self.lib.atomo_embedding(self._h, table.data_ptr(), code, rows, cols, ld, ids.data_ptr(), width, n, scale, out.data_ptr(), ld_out,
+                                      self._status(status), self._own_stream(stream))
+        self._check(rc, "atomo_embedding")
+        return out
+
+    def atomo_embedding_backward(self, ids: torch.Tensor, grad: torch.Tensor, rows: int, scale: float = 1.0, padding_idx: int = -1,
+                                 out: Optional[torch.Tensor] = None, accumulate: bool = False, status: Optional[torch.Tensor] = None,
+                                 stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+        """The gradient of a table of `rows` rows, fp32: row v is scale times the sum of grad over the tokens of id v, in the order of the
+        tokens.  grad: ids.shape + (cols,).  out: a matrix to write to, or with accumulate=True to add to.  Tokens of padding_idx (-1: none) are left out."""
+        code = TYPE_CODES[self._operand(grad, "grad").dtype]
+        width = self._ids(ids)
+        if grad.dim() < 1 or grad.shape[:-1] != ids.shape:
+            raise ValueError("grad: the shape of ids with one more dimension is required")
+        n, cols = ids.numel(), grad.shape[-1]
+        _, ld = _rows(grad, cols, "grad") if n and cols else (0, max(cols, 1))
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate needs out")
+            out = torch.empty((rows, cols), dtype=torch.float32, device=grad.device)
+            ld_out = cols
+        else:
+            n_out, ld_out = _rows(self._operand(out, "out", (torch.float32,)), cols, "out")
+            if n_out != rows:
+                raise ValueError(f"out: {rows} rows are required")
+        s = self._own_stream(stream)
+        nbytes = int(self.lib.atomo_embedding_workspace_bytes(n, rows, cols))
+        if nbytes < 0:
+            raise AtomoError(1, "atomo_embedding_workspace_bytes")
+        ws = self._scratch(nbytes, stream)
+        rc = self.lib.atomo_embedding_backward(self._h, ids.data_ptr(), width, n, grad.data_ptr(), code, ld, rows, cols, scale, padding_idx, out.data_ptr(), ld_out,
+                                               1 if accumulate else 0, self._status(status), ws.data_ptr(), nbytes, s)
+        self._check(rc, "atomo_embedding_backward")
+        return out
+
+    def _weight(self, weight, bias, cols: int):
+        """(pointers of weight and bias, type code) of a layer norm's parameters, either of which may be None."""
+        kinds = {t.dtype for t in (weight, bias) if t is not None}
+        if len(kinds) > 1:
+            raise ValueError("weight and bias must have one type")
+        for name, t in (("weight", weight), ("bias", bias)):
+            if t is not None and not (self._operand(t, name).is_contiguous() and t.numel() == cols):
+                raise ValueError(f"{name}: a contiguous tensor of {cols} elements is required")
+        ptr = lambda t: None if t is None else t.data_ptr()
+        return ptr(weight), ptr(bias), TYPE_CODES[kinds.pop()] if kinds else 0
+
+    def atomo_layer_norm(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                         out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+        """Layer norm over the last dimension: (y, mean, rstd), y of x's type and shape, mean and rstd in fp32 with one value per row.  out may
+        be x."""
+        code = TYPE_CODES[self._operand(x, "x").dtype]
+        cols = x.shape[-1] if x.dim() else 0
+        rows, ld = _rows(x, cols, "x") if x.numel() else (0, max(cols, 1))
+        w, b, wcode = self._weight(weight, bias, cols)
+        if out is None:
+            out, ld_out = torch.empty(x.shape, dtype=x.dtype, device=x.device), cols
+        else:
+            if self._operand(out, "out", (x.dtype,)).shape != x.shape:
+                raise ValueError("out: the shape of x is required")
+            _, ld_out = _rows(out, cols, "out") if x.numel() else (0, max(cols, 1))
+        stats = torch.empty((2, *x.shape[:-1]), dtype=torch.float32, device=x.device)
+        mean, rstd = stats.unbind(0)
+        rc = self.lib.atomo_layer_norm(self._h, x.data_ptr(), code, rows, cols, ld, w, b, wcode, eps, out.data_ptr(), ld_out, mean.data_ptr(), rstd.data_ptr(),
+                                       self._own_stream(stream))
+        self._check(rc, "atomo_layer_norm")
+        return out, mean, rstd
+
+    def atomo_layer_norm_backward(self, dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                                  out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+        """(dx, dweight, dbias) of atomo_layer_norm: dx of x's type, dweight and dbias in fp32, whatever the weight's type.  out (for dx) may
+        be dy or x."""
+        code = TYPE_CODES[self._operand(x, "x").dtype]
+        self._operand(dy, "dy", (x.dtype,))
+        cols = x.shape[-1] if x.dim() else 0
+        if dy.shape != x.shape:
+            raise ValueError("dy: the shape of x is required")
+        rows, ld = _rows(x, cols, "x") if x.numel() else (0, max(cols, 1))
+        _, ld_dy = _rows(dy, cols, "dy") if x.numel() else (0, max(cols, 1))
+        for name, t in (("mean", mean), ("rstd", rstd)):
+            if not (self._operand(t, name, (torch.float32,)).is_contiguous() and t.numel() == rows):
+                raise ValueError(f"{name}: {rows} contiguous fp32 numbers are required")
+        w, _, wcode = self._weight(weight, None, cols)
+        if out is None:
+            out, ld_dx = torch.empty(x.shape, dtype=x.dtype, device=x.device), max(cols, 1)
+        else:
+            if self._operand(out, "out", (x.dtype,)).shape != x.shape:
+                raise ValueError("out: the shape of x is required")
+            _, ld_dx = _rows(out, cols, "out") if x.numel() else (0, max(cols, 1))
+        dweight, dbias = torch.empty((2, cols), dtype=torch.float32, device=x.device).unbind(0)
+        s = self._own_stream(stream)
+        nbytes = int(self.lib.atomo_layer_norm_workspace_bytes(rows, cols))
+        if nbytes < 0:
+            raise AtomoError(1, "atomo_layer_norm_workspace_bytes")
+        ws = self._scratch(nbytes, stream)
+        rc = self.lib.atomo_layer_norm_backward(self._h, dy.data_ptr(), ld_dy, x.data_ptr(), ld, code, rows, cols, w, wcode, mean.data_ptr(), rstd.data_ptr(),
+                                                out.data_ptr(), ld_dx, dweight.data_ptr(), dbias.data_ptr(), ws.data_ptr(), nbytes, s)
+        self._check(rc, "atomo_layer_norm_backward")
+        return out, dweight, dbias
 
     def read_headers(self, payload: Payload, stream: Optional[torch.cuda.Stream] = None):
         gh = PayloadHeader()

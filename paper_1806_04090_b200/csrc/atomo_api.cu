@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "atomo_kernels.cuh"
+#include "atomo_ops.cuh"
 
 using namespace atomo;
 
@@ -354,6 +355,37 @@ int side_stream(atomo_ctx* ctx, cudaStream_t st, cudaStream_t* out) {
 }
 
 bool bad_budget(double s) { return !(s > 0.0) || !std::isfinite(s); }
+
+
+// ---- operators on either side of the exchange: checks, the device of a call
+struct DeviceScope {                 // the context's device for the call, the caller's again afterwards
+  int before = -1; bool changed = false; cudaError_t err = cudaSuccess;
+  explicit DeviceScope(int device) {
+    err = cudaGetDevice(&before);
+    if (err == cudaSuccess && before != device) { err = cudaSetDevice(device); changed = err == cudaSuccess; }
+  }
+  ~DeviceScope() { if (changed) cudaSetDevice(before); }
+};
+bool bad_type(int type) { return type < ATOMO_TYPE_F32 || type > ATOMO_TYPE_F16; }
+bool off_type(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
+// null, or not aligned to its elements
+bool bad_ptr(const void* p, int bytes) { return !p || off_type(p, bytes); }
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1, kMostCols = (int64_t)1 << 24;
+// rows x cols with a leading dimension: offsets stay within 62 bits
+bool bad_shape(int64_t rows, int64_t cols, int64_t ld) { return rows < 0 || rows > kMostRows || cols <= 0 || cols > kMostCols || ld < cols || ld > (int64_t)1 << 31; }
+// runs f on the context's device; nothing is thrown through the C boundary
+template <typename F> int on_device(atomo_ctx* ctx, const char* what, F f) {
+  try {
+    DeviceScope scope(ctx->device);
+    if (scope.err != cudaSuccess) return fail_cuda(ctx, scope.err, "cudaSetDevice");
+    const cudaError_t e = (cudaError_t)f();
+    if (e == cudaSuccess) return ATOMO_OK;
+    cudaGetLastError();              // a launch that was refused is reported here, not by the next call
+    return fail_cuda(ctx, e, what);
+  } catch (...) {
+    return ATOMO_ERR_CUDA;           // no host memory
+  }
+}
 
 }  // namespace
 
@@ -1465,6 +1497,98 @@ int atomo_decode_average(atomo_ctx* ctx, int32_t kind, const void* const* payloa
   }
   CK(cudaGetLastError());
   return ATOMO_OK;
+}
+
+// ==================================================================================================
+// Operators on either side of the exchange.  They use nothing of the context but its device and its error text.
+
+int64_t atomo_grad_norm_workspace_bytes(void) { return (int64_t)kNormSlots * sizeof(double); }
+
+int atomo_grad_norm(atomo_ctx* ctx, const atomo_tensor* grads, int32_t n_tensors, double max_norm, float* out, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!ctx || !grads || n_tensors <= 0 || n_tensors > 1 << 20 || !(max_norm > 0.0) || bad_ptr(out, 4)) return ATOMO_ERR_INVALID_ARG;
+  for (int i = 0; i < n_tensors; ++i) {
+    const atomo_tensor& t = grads[i];
+    if (t.n < 0 || t.n > (int64_t)1 << 40 || bad_type(t.type) || (t.n > 0 && bad_ptr(t.data, type_bytes(t.type)))) return ATOMO_ERR_INVALID_ARG;
+  }
+  if (bad_ptr(workspace, 8)) return ATOMO_ERR_INVALID_ARG;
+  if (workspace_bytes < atomo_grad_norm_workspace_bytes()) return ATOMO_ERR_CAPACITY;
+  return on_device(ctx, "gradient norm", [&] { return launch_grad_norm(grads, n_tensors, max_norm, out, static_cast<double*>(workspace), (cudaStream_t)stream); });
+}
+
+int atomo_adamw(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, const void* const* grads, int32_t n_tensors, const atomo_adamw_args* args, void* stream) {
+  if (!ctx || !tensors || !grads || n_tensors <= 0 || !args) return ATOMO_ERR_INVALID_ARG;
+  const atomo_adamw_args& a = *args;
+  if (!(a.lr >= 0.0) || !std::isfinite(a.lr) || !(a.eps >= 0.0) || !std::isfinite(a.eps) || !(a.beta1 >= 0.0 && a.beta1 < 1.0) || !(a.beta2 >= 0.0 && a.beta2 < 1.0) || a.step < 1)
+    return ATOMO_ERR_INVALID_ARG;
+  if ((a.state_bits != 32 && a.state_bits != 8) || bad_type(a.grad_type) || off_type(a.scale, 4)) return ATOMO_ERR_INVALID_ARG;
+  const bool small = a.state_bits == 8;
+  for (int i = 0; i < n_tensors; ++i) {
+    const atomo_adamw_tensor& t = tensors[i];
+    if (t.n < 0 || t.n >= (small ? (int64_t)1 << 34 : (int64_t)1 << 40) || bad_type(t.type) || !(t.weight_decay >= 0.0f) || !std::isfinite(t.weight_decay)) return ATOMO_ERR_INVALID_ARG;
+    if (t.n == 0) continue;
+    if (bad_ptr(t.param, type_bytes(t.type)) || bad_ptr(grads[i], type_bytes(a.grad_type)) || off_type(t.master, 4)) return ATOMO_ERR_INVALID_ARG;
+    if (bad_ptr(t.exp_avg, small ? 1 : 4) || bad_ptr(t.exp_avg_sq, small ? 1 : 4) || (small && (!t.exp_avg_scale || !t.exp_avg_sq_scale))) return ATOMO_ERR_INVALID_ARG;
+  }
+  AdamHyper h;
+  h.beta1 = (float)a.beta1; h.one_minus_beta1 = (float)(1.0 - a.beta1); h.beta2 = (float)a.beta2; h.one_minus_beta2 = (float)(1.0 - a.beta2);
+  h.lr = (float)a.lr; h.eps = (float)a.eps;
+  h.step_size = (float)(a.lr / (1.0 - std::pow(a.beta1, (double)a.step)));
+  h.inv_root_bias2 = (float)(1.0 / std::sqrt(1.0 - std::pow(a.beta2, (double)a.step)));
+  h.scale = a.scale; h.step = (uint32_t)a.step; h.grad_type = a.grad_type;
+  h.key = PhiloxKey{(uint32_t)a.seed, (uint32_t)(a.seed >> 32)};
+  return on_device(ctx, "adamw", [&] { return launch_adamw(tensors, grads, n_tensors, a.state_bits, h, (cudaStream_t)stream); });
+}
+
+int atomo_embedding(atomo_ctx* ctx, const void* table, int32_t type, int64_t rows, int64_t cols, int64_t ld, const void* ids, int32_t id_bytes, int64_t n_ids,
+                    double scale, void* out, int64_t ld_out, int32_t* status, void* stream) {
+  if (!ctx || bad_type(type) || rows <= 0 || bad_shape(rows, cols, ld) || bad_shape(n_ids, cols, ld_out) || (id_bytes != 4 && id_bytes != 8)) return ATOMO_ERR_INVALID_ARG;
+  if (!std::isfinite(scale) || bad_ptr(table, type_bytes(type)) || off_type(status, 4)) return ATOMO_ERR_INVALID_ARG;
+  if (n_ids > 0 && (bad_ptr(ids, id_bytes) || bad_ptr(out, type_bytes(type)))) return ATOMO_ERR_INVALID_ARG;
+  const EmbLookup a{table, type, rows, cols, ld, ids, id_bytes, n_ids, (float)scale, out, ld_out, status};
+  return on_device(ctx, "embedding", [&] { return launch_embedding(a, (cudaStream_t)stream); });
+}
+
+int64_t atomo_embedding_workspace_bytes(int64_t n_ids, int64_t rows, int64_t cols) {
+  if (rows <= 0 || bad_shape(rows, cols, cols) || n_ids < 0 || n_ids > kMostRows) return -1;
+  return (int64_t)embedding_workspace(n_ids, rows, cols);
+}
+
+int atomo_embedding_backward(atomo_ctx* ctx, const void* ids, int32_t id_bytes, int64_t n_ids, const void* grad, int32_t type, int64_t ld, int64_t rows, int64_t cols,
+                             double scale, int64_t padding_idx, float* out, int64_t ld_out, int32_t accumulate, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!ctx || bad_type(type) || rows <= 0 || bad_shape(rows, cols, ld_out) || bad_shape(n_ids, cols, ld) || (id_bytes != 4 && id_bytes != 8)) return ATOMO_ERR_INVALID_ARG;
+  if (!std::isfinite(scale) || bad_ptr(out, 4) || off_type(status, 4) || padding_idx < -1 || padding_idx >= rows) return ATOMO_ERR_INVALID_ARG;
+  if (n_ids > 0 && (bad_ptr(ids, id_bytes) || bad_ptr(grad, type_bytes(type)))) return ATOMO_ERR_INVALID_ARG;
+  const int64_t need = atomo_embedding_workspace_bytes(n_ids, rows, cols);
+  if (bad_ptr(workspace, 16)) return ATOMO_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return ATOMO_ERR_CAPACITY;
+  const EmbBackward a{ids, id_bytes, n_ids, grad, type, ld, rows, cols, (float)scale, padding_idx, out, ld_out, accumulate != 0, status, static_cast<uint8_t*>(workspace)};
+  return on_device(ctx, "embedding gradient", [&] { return launch_embedding_backward(a, (cudaStream_t)stream); });
+}
+
+int atomo_layer_norm(atomo_ctx* ctx, const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ld, const void* weight, const void* bias, int32_t weight_type,
+                     double eps, void* y, int64_t ld_y, float* mean, float* rstd, void* stream) {
+  if (!ctx || bad_type(type) || bad_type(weight_type) || bad_shape(rows, cols, ld) || bad_shape(rows, cols, ld_y) || !(eps >= 0.0) || !std::isfinite(eps)) return ATOMO_ERR_INVALID_ARG;
+  if (off_type(weight, type_bytes(weight_type)) || off_type(bias, type_bytes(weight_type))) return ATOMO_ERR_INVALID_ARG;
+  if (rows > 0 && (bad_ptr(x, type_bytes(type)) || bad_ptr(y, type_bytes(type)) || bad_ptr(mean, 4) || bad_ptr(rstd, 4))) return ATOMO_ERR_INVALID_ARG;
+  const NormForward a{x, type, rows, cols, ld, weight, bias, weight_type, (float)eps, y, ld_y, mean, rstd};
+  return on_device(ctx, "layer norm", [&] { return launch_layer_norm(a, (cudaStream_t)stream); });
+}
+
+int64_t atomo_layer_norm_workspace_bytes(int64_t rows, int64_t cols) {
+  if (bad_shape(rows, cols, cols)) return -1;
+  return (int64_t)layer_norm_workspace(rows, cols);
+}
+
+int atomo_layer_norm_backward(atomo_ctx* ctx, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int32_t type, int64_t rows, int64_t cols, const void* weight,
+                              int32_t weight_type, const float* mean, const float* rstd, void* dx, int64_t ld_dx, float* dweight, float* dbias,
+                              void* workspace, int64_t workspace_bytes, void* stream) {
+  if (!ctx || bad_type(type) || bad_type(weight_type) || bad_shape(rows, cols, ld_dy) || bad_shape(rows, cols, ld_x) || bad_shape(rows, cols, ld_dx)) return ATOMO_ERR_INVALID_ARG;
+  if (off_type(weight, type_bytes(weight_type)) || off_type(dweight, 4) || off_type(dbias, 4)) return ATOMO_ERR_INVALID_ARG;
+  const int size = type_bytes(type);
+  if (rows > 0 && (bad_ptr(dy, size) || bad_ptr(x, size) || bad_ptr(dx, size) || bad_ptr(mean, 4) || bad_ptr(rstd, 4) || bad_ptr(workspace, 16))) return ATOMO_ERR_INVALID_ARG;
+  if (workspace_bytes < atomo_layer_norm_workspace_bytes(rows, cols)) return ATOMO_ERR_CAPACITY;
+  const NormBackward a{dy, x, type, rows, cols, ld_dy, ld_x, weight, weight_type, mean, rstd, dx, ld_dx, dweight, dbias, static_cast<float*>(workspace)};
+  return on_device(ctx, "layer norm gradient", [&] { return launch_layer_norm_backward(a, (cudaStream_t)stream); });
 }
 
 // ==================================================================================================

@@ -1,0 +1,94 @@
+// Descriptors and launchers of the operators on either side of the gradient exchange (gradient norm, AdamW, embedding, layer norm),
+// and what their kernels share: values of three types in 32-bit arithmetic, launches that overlap their predecessor's end.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <string.h>
+
+#include <vector>
+
+#include "atomo_common.cuh"
+
+namespace atomo {
+
+__host__ __device__ __forceinline__ int type_bytes(int type) { return type == ATOMO_TYPE_F32 ? 4 : 2; }
+
+// ---- values ---------------------------------------------------------------------------------------
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+
+// V neighbouring values, moved in one piece
+template <typename T, int V> struct alignas(V * sizeof(T)) Pack { T v[V]; };
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_pack(const T* p) { return *reinterpret_cast<const Pack<T, V>*>(p); }
+template <typename T, int V> __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& x) { *reinterpret_cast<Pack<T, V>*>(p) = x; }
+
+// ---- launches -------------------------------------------------------------------------------------
+// A kernel launched with launch_after() may start while the kernel before it in the stream ends; it calls wait_for_previous() in every
+// thread before it touches memory.
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A... args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
+// ---- gradient norm (atomo_step.cu) ----------------------------------------------------------------
+// most partial sums of a call, 8 bytes each
+constexpr int kNormSlots = 148 * 8;
+int launch_grad_norm(const atomo_tensor* grads, int n, double max_norm, float* out, double* slots, cudaStream_t st);   // cudaError_t
+
+// ---- AdamW (atomo_step.cu) ------------------------------------------------------------------------
+struct AdamHyper {
+  float beta1, one_minus_beta1, beta2, one_minus_beta2;
+  float lr, step_size, inv_root_bias2, eps;   // step_size = lr / (1 - beta1^t), inv_root_bias2 = 1 / sqrt(1 - beta2^t)
+  const float* scale;                         // DEVICE: {norm, factor of the gradient}, or null
+  uint32_t step; int32_t grad_type;
+  PhiloxKey key;
+};
+int launch_adamw(const atomo_adamw_tensor* tensors, const void* const* grads, int n, int bits, const AdamHyper& h, cudaStream_t st);   // cudaError_t
+
+// ---- embedding (atomo_embedding.cu) ---------------------------------------------------------------
+constexpr int kEmbChunk = 32;           // sorted tokens that are summed by one group of threads
+struct EmbLookup {
+  const void* table; int type; int64_t rows, cols, ld;
+  const void* ids; int id_bytes; int64_t n;
+  float scale; void* out; int64_t ld_out; int32_t* status;
+};
+struct EmbBackward {
+  const void* ids; int id_bytes; int64_t n;
+  const void* grad; int type; int64_t ld, rows, cols;
+  float scale; int64_t padding;         // id whose tokens are left out, or -1
+  float* out; int64_t ld_out; int accumulate; int32_t* status;
+  uint8_t* ws;
+};
+int launch_embedding(const EmbLookup& a, cudaStream_t st);                       // cudaError_t
+uint64_t embedding_workspace(int64_t n, int64_t rows, int64_t cols);
+int launch_embedding_backward(const EmbBackward& a, cudaStream_t st);            // cudaError_t
+
+// ---- layer norm (atomo_layernorm.cu) --------------------------------------------------------------
+struct NormForward {
+  const void* x; int type; int64_t rows, cols, ld;
+  const void *weight, *bias; int weight_type; float eps;
+  void* y; int64_t ld_y; float *mean, *rstd;
+};
+struct NormBackward {
+  const void *dy, *x; int type; int64_t rows, cols, ld_dy, ld_x;
+  const void* weight; int weight_type; const float *mean, *rstd;
+  void* dx; int64_t ld_dx; float *dweight, *dbias;
+  float* ws;
+};
+int launch_layer_norm(const NormForward& a, cudaStream_t st);                    // cudaError_t
+uint64_t layer_norm_workspace(int64_t rows, int64_t cols);
+int launch_layer_norm_backward(const NormBackward& a, cudaStream_t st);          // cudaError_t
+
+}  // namespace atomo

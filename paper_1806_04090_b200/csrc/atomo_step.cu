@@ -1,0 +1,453 @@
+// The parameter update behind the gradient exchange: global norm of a list of gradients, AdamW over a list of parameters.
+//
+// Both are one pass over memory.  The tensors of a call travel as kernel arguments (up to 32 KB of them), so that a call needs no table
+// in device memory; a CTA finds the tensor of its chunk by bisection over the tensors' first chunks.
+#include <algorithm>
+
+#include "atomo_ops.cuh"
+
+namespace atomo {
+namespace {
+
+// =================================== norm ========================================================
+// sqrt(sum g^2).  Squares are summed in fp32 over the 16 or 32 values that a thread has in registers and in fp64 from there on.  Where
+// such a sum is not well inside the range of fp32 (values around 1e19 or 1e-14 and beyond, all of them zero, NaN or Inf) it is
+// formed again in fp64 from the registers: the norm neither overflows nor loses small gradients, and rounds to fp32 once, at the end.
+constexpr int kNormThreads = 256, kNormLoads = 4;
+constexpr int kNormChunk = kNormThreads * kNormLoads * 16;     // bytes per step of a CTA
+constexpr int kNormCluster = 8;
+
+struct NormTensor { const uint8_t* data; int64_t n; uint32_t chunk0; int32_t type; };   // chunk0: first chunk in the launch
+template <int N> struct NormBatch {
+  NormTensor t[N];
+  int n; uint32_t chunks; int slot0;
+  double max_norm; double* slots; float* out;
+};
+
+__device__ __forceinline__ void square_pair(uint32_t w, int type, float& a, float& b) {
+  if (type == ATOMO_TYPE_BF16) { a = __uint_as_float(w << 16); b = __uint_as_float(w & 0xffff0000u); }
+  else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); a = f.x; b = f.y; }
+}
+__device__ __forceinline__ bool sum_holds(float s) { return s > 1.0e-27f && s < 1.0e37f; }
+
+__device__ __forceinline__ double norm_value(const NormTensor& t, int64_t i) {
+  if (t.type == ATOMO_TYPE_F32) return (double)reinterpret_cast<const float*>(t.data)[i];
+  if (t.type == ATOMO_TYPE_BF16) return (double)to_float(reinterpret_cast<const __nv_bfloat16*>(t.data)[i]);
+  return (double)to_float(reinterpret_cast<const __half*>(t.data)[i]);
+}
+
+// squares of what a thread holds of one chunk; zeros count for nothing
+__device__ __forceinline__ double norm_chunk(const uint4 (&r)[kNormLoads], int type) {
+  float s = 0.0f;
+  if (type == ATOMO_TYPE_F32) {
+#pragma unroll
+    for (int j = 0; j < kNormLoads; ++j) {
+      const float* f = reinterpret_cast<const float*>(&r[j]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s = fmaf(f[k], f[k], s);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < kNormLoads; ++j) {
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(&r[j]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { float a, b; square_pair(w[k], type, a, b); s = fmaf(a, a, s); s = fmaf(b, b, s); }
+    }
+  }
+  if (sum_holds(s)) return (double)s;
+  double d = 0.0;
+#pragma unroll
+  for (int j = 0; j < kNormLoads; ++j) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&r[j]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float a = __uint_as_float(w[k]), b = 0.0f;
+      if (type != ATOMO_TYPE_F32) square_pair(w[k], type, a, b);
+      d = fma((double)a, (double)a, d); d = fma((double)b, (double)b, d);
+    }
+  }
+  return d;
+}
+
+__device__ __forceinline__ void norm_finish(double sum, double max_norm, float* out) {
+  const double norm = sqrt(sum);
+  out[0] = (float)norm;
+  // a norm that is not finite gives a factor that is none: atomo_adamw then leaves the parameters as they are
+  out[1] = norm <= 1.7e308 ? (float)fmin(1.0, max_norm / (norm + 1e-6)) : __int_as_float(0x7fc00000);
+}
+
+__device__ __forceinline__ double block_sum(double v, double* s_warp) {
+  v = warp_sum(v);
+  if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = v;
+  __syncthreads();
+  double t = 0.0;
+  if (threadIdx.x < 32) {
+    t = threadIdx.x < (blockDim.x >> 5) ? s_warp[threadIdx.x] : 0.0;
+    t = warp_sum(t);
+  }
+  return t;                                                      // valid in warp 0
+}
+
+// A CTA takes a contiguous run of the launch's chunks.  ONE: the launch is one cluster, whose first CTA adds the others' sums through
+// distributed shared memory; else the sums go to slots that norm_join_kernel adds.
+template <int N, bool ONE>
+__global__ void __launch_bounds__(kNormThreads) norm_kernel(const __grid_constant__ NormBatch<N> B) {
+  __shared__ double s_warp[kNormThreads / 32];
+  __shared__ double s_ctas[kNormCluster];
+  const uint32_t per = (B.chunks + gridDim.x - 1) / gridDim.x;
+  const uint32_t first = blockIdx.x * per, last = min(first + per, B.chunks);
+  double acc = 0.0;
+  if (first < last) {
+    int lo = 0, hi = B.n - 1;                                    // the last tensor that starts at or before `first`
+    while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (B.t[mid].chunk0 <= first) lo = mid; else hi = mid - 1; }
+    NormTensor t = B.t[lo];
+    uint32_t end = lo + 1 < B.n ? B.t[lo + 1].chunk0 : B.chunks;
+    for (uint32_t c = first; c < last; ++c) {
+      if (c >= end) { ++lo; t = B.t[lo]; end = lo + 1 < B.n ? B.t[lo + 1].chunk0 : B.chunks; }
+      const int size = type_bytes(t.type);
+      // the values before the first 16-byte boundary and behind the last one are taken one by one, by the tensor's first chunk
+      const int64_t head = min(t.n, (int64_t)(((16u - (uint32_t)(reinterpret_cast<uintptr_t>(t.data) & 15u)) & 15u) / size));
+      const int64_t packs = (t.n - head) * size / 16, tail = t.n - head - packs * (16 / size);
+      const uint8_t* body = t.data + head * size;
+      const int64_t at = (int64_t)(c - t.chunk0) * (kNormThreads * kNormLoads) + threadIdx.x;
+      uint4 r[kNormLoads];
+#pragma unroll
+      for (int j = 0; j < kNormLoads; ++j) {
+        const int64_t i = at + j * kNormThreads;
+        r[j] = i < packs ? *reinterpret_cast<const uint4*>(body + i * 16) : make_uint4(0u, 0u, 0u, 0u);
+      }
+      acc += norm_chunk(r, t.type);
+      if (c == t.chunk0 && threadIdx.x < head + tail) {
+        const double x = norm_value(t, threadIdx.x < head ? threadIdx.x : t.n - tail + (threadIdx.x - head));
+        acc = fma(x, x, acc);
+      }
+    }
+  }
+  const double sum = block_sum(acc, s_warp);
+  if constexpr (ONE) {
+    if (threadIdx.x == 0) {
+      uint32_t remote, local = (uint32_t)__cvta_generic_to_shared(&s_ctas[blockIdx.x]);
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(0));
+      asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(remote), "d"(sum) : "memory");
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+      double all = 0.0;
+      for (uint32_t k = 0; k < gridDim.x; ++k) all += s_ctas[k];
+      norm_finish(all, B.max_norm, B.out);
+    }
+  } else {
+    if (threadIdx.x == 0) B.slots[B.slot0 + blockIdx.x] = sum;
+  }
+}
+
+__global__ void __launch_bounds__(kNormThreads) norm_join_kernel(const double* __restrict__ slots, int n, double max_norm, float* __restrict__ out) {
+  __shared__ double s_warp[kNormThreads / 32];
+  wait_for_previous();
+  double acc = 0.0;
+  for (int i = threadIdx.x; i < n; i += kNormThreads) acc += slots[i];
+  const double sum = block_sum(acc, s_warp);
+  if (threadIdx.x == 0) norm_finish(sum, max_norm, out);
+}
+
+uint64_t norm_chunks(const atomo_tensor& t) {                   // upper bound that the kernel's own split never exceeds
+  return std::max<uint64_t>(1, ((uint64_t)t.n * type_bytes(t.type) + kNormChunk - 1) / kNormChunk);
+}
+
+template <int N>
+cudaError_t norm_launch(NormBatch<N>& B, int grid, bool one, cudaStream_t st) {
+  if (!one) { norm_kernel<N, false><<<grid, kNormThreads, 0, st>>>(B); return cudaGetLastError(); }
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = grid; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(kNormThreads); cfg.stream = st;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, norm_kernel<N, true>, B);
+}
+
+template <int N>
+cudaError_t norm_batch(const atomo_tensor* g, const int* index, int n, int grid, bool one, int slot0, double max_norm, float* out, double* slots, cudaStream_t st) {
+  NormBatch<N> B;
+  uint64_t at = 0;
+  for (int i = 0; i < n; ++i) {
+    const atomo_tensor& t = g[index[i]];
+    B.t[i] = NormTensor{static_cast<const uint8_t*>(t.data), t.n, (uint32_t)at, t.type};
+    at += norm_chunks(t);
+  }
+  B.n = n; B.chunks = (uint32_t)at; B.slot0 = slot0; B.max_norm = max_norm; B.slots = slots; B.out = out;
+  return norm_launch<N>(B, grid, one, st);
+}
+
+__global__ void norm_empty_kernel(double max_norm, float* out) { norm_finish(0.0, max_norm, out); }
+
+}  // namespace
+
+int launch_grad_norm(const atomo_tensor* grads, int n, double max_norm, float* out, double* slots, cudaStream_t st) {
+  constexpr int kMost = 1024;                                    // 24 bytes each: 24 KB of kernel arguments
+  std::vector<int> index;
+  uint64_t chunks = 0;
+  for (int i = 0; i < n; ++i) if (grads[i].n > 0) { index.push_back(i); chunks += norm_chunks(grads[i]); }
+  const int m = (int)index.size();
+  if (m == 0) { norm_empty_kernel<<<1, 1, 0, st>>>(max_norm, out); return (int)cudaGetLastError(); }
+  // A few chunks: one cluster does it all.
+  if (m <= kMost && chunks <= 8 * kNormCluster) {
+    const int grid = (int)std::min<uint64_t>(chunks, kNormCluster);
+    if (m <= 8) return (int)norm_batch<8>(grads, index.data(), m, grid, true, 0, max_norm, out, slots, st);
+    if (m <= 128) return (int)norm_batch<128>(grads, index.data(), m, grid, true, 0, max_norm, out, slots, st);
+    return (int)norm_batch<kMost>(grads, index.data(), m, grid, true, 0, max_norm, out, slots, st);
+  }
+  const int launches = (m + kMost - 1) / kMost;
+  int used = 0;
+  for (int l = 0; l < launches; ++l) {
+    const int i0 = l * kMost, count = std::min(kMost, m - i0);
+    uint64_t part = 0;
+    for (int i = i0; i < i0 + count; ++i) part += norm_chunks(grads[index[i]]);
+    // the slots are shared out evenly: a call of more than kNormSlots * kMost tensors is refused before it gets here
+    const int grid = (int)std::min<uint64_t>(part, (uint64_t)kNormSlots / launches);
+    const cudaError_t e = count <= 8 ? norm_batch<8>(grads, &index[i0], count, grid, false, used, max_norm, out, slots, st)
+                        : count <= 128 ? norm_batch<128>(grads, &index[i0], count, grid, false, used, max_norm, out, slots, st)
+                                       : norm_batch<kMost>(grads, &index[i0], count, grid, false, used, max_norm, out, slots, st);
+    if (e != cudaSuccess) return (int)e;
+    used += grid;
+  }
+  return (int)launch_after(norm_join_kernel, dim3(1), dim3(kNormThreads), 0, st, slots, used, max_norm, out);
+}
+
+namespace {
+
+// =================================== AdamW =======================================================
+// m = b1 m + (1 - b1) c g,  v = b2 v + (1 - b2) (c g)^2,  p = p - lr wd p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps),
+// all in fp32; c is read from device memory.  A thread takes four neighbouring elements kAdamGroups times, all loads first.
+constexpr int kAdamThreads = 256, kAdamGroups = 4;
+constexpr int kAdamChunk = kAdamThreads * 4 * kAdamGroups;
+constexpr int kStateBlock = ATOMO_STATE_BLOCK;
+
+struct AdamTensor {
+  void* p; const void* g; void* m; void* v; uint8_t* ms; uint8_t* vs; float* master;
+  int64_t n; float decay; int32_t type; uint32_t index, vec;     // vec: every array may be moved four elements at a time
+};
+template <int N> struct AdamBatch {
+  AdamTensor t[N];
+  uint32_t chunk0[N];
+  int n; AdamHyper h;
+};
+
+// four elements of `size` bytes each as they lie in memory, in the low words of r; `count` of them exist
+__device__ __forceinline__ uint4 load_raw4(const void* base, int size, int64_t e, int count, bool vec) {
+  uint4 r = make_uint4(0u, 0u, 0u, 0u);
+  const uint8_t* p = static_cast<const uint8_t*>(base) + e * size;
+  if (vec && count >= 4) {
+    if (size == 4) r = *reinterpret_cast<const uint4*>(p);
+    else if (size == 2) { const uint2 q = *reinterpret_cast<const uint2*>(p); r.x = q.x; r.y = q.y; }
+    else r.x = *reinterpret_cast<const uint32_t*>(p);
+    return r;
+  }
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (j < count) {
+      if (size == 4) w[j] = reinterpret_cast<const uint32_t*>(p)[j];
+      else if (size == 2) w[j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
+      else w[0] |= (uint32_t)p[j] << (8 * j);
+    }
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store_raw4(void* base, int size, int64_t e, int count, bool vec, uint4 r) {
+  uint8_t* p = static_cast<uint8_t*>(base) + e * size;
+  if (vec && count >= 4) {
+    if (size == 4) *reinterpret_cast<uint4*>(p) = r;
+    else if (size == 2) *reinterpret_cast<uint2*>(p) = make_uint2(r.x, r.y);
+    else *reinterpret_cast<uint32_t*>(p) = r.x;
+    return;
+  }
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (j < count) {
+      if (size == 4) reinterpret_cast<uint32_t*>(p)[j] = w[j];
+      else if (size == 2) reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+      else p[j] = (uint8_t)(w[0] >> (8 * j));
+    }
+  }
+}
+__device__ __forceinline__ void unpack4(uint4 r, int type, float (&x)[4]) {
+  if (type == ATOMO_TYPE_F32) { x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w); }
+  else if (type == ATOMO_TYPE_BF16) {
+    x[0] = __uint_as_float(r.x << 16); x[1] = __uint_as_float(r.x & 0xffff0000u);
+    x[2] = __uint_as_float(r.y << 16); x[3] = __uint_as_float(r.y & 0xffff0000u);
+  } else {
+    const float2 a = __half22float2(*reinterpret_cast<__half2*>(&r.x)), b = __half22float2(*reinterpret_cast<__half2*>(&r.y));
+    x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+  }
+}
+// to the nearest value of the type, ties to even
+__device__ __forceinline__ uint4 pack4(const float (&x)[4], int type) {
+  uint4 r = make_uint4(0u, 0u, 0u, 0u);
+  if (type == ATOMO_TYPE_F32) r = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  else if (type == ATOMO_TYPE_BF16) {
+    __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+    r.x = *reinterpret_cast<uint32_t*>(&a); r.y = *reinterpret_cast<uint32_t*>(&b);
+  } else {
+    __half2 a = __floats2half2_rn(x[0], x[1]), b = __floats2half2_rn(x[2], x[3]);
+    r.x = *reinterpret_cast<uint32_t*>(&a); r.y = *reinterpret_cast<uint32_t*>(&b);
+  }
+  return r;
+}
+
+// A state in 8 bits: e4m3 codes times a power of two for each 32 neighbouring elements, kept as its exponent byte.
+__device__ __forceinline__ float state_scale(uint32_t byte) { return __uint_as_float(byte > 0u ? byte << 23 : 0x00400000u); }
+__device__ __forceinline__ void state_decode(uint32_t codes, uint32_t byte, float (&x)[4]) {
+  uint32_t lo, hi;
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(codes));
+  const float s = state_scale(byte);
+  const float2 a = __half22float2(*reinterpret_cast<__half2*>(&lo)), b = __half22float2(*reinterpret_cast<__half2*>(&hi));
+  x[0] = a.x * s; x[1] = a.y * s; x[2] = b.x * s; x[3] = b.y * s;
+}
+// The power of two brings the block's largest finite magnitude into [224, 448), so that rounding it up stays within e4m3.  The magnitude
+// times 2^-120 has e4m3's exponent in the exponent field of fp32, subnormal numbers included, so that its code is the upper 12 of
+// the 32 bits; 16 random bits added below them round up with the probability of what is cut off (to 2^-16 of a step).
+// above_zero: a value above zero is never rounded to zero (a second moment of zero beside a first moment that is not would make a
+// step of any size).  What is not finite becomes NaN.
+__device__ __forceinline__ uint32_t state_encode(const float (&x)[4], const uint32_t (&random)[4], bool above_zero, uint32_t& byte) {
+  uint32_t mag[4], top = 0u, wild = 0u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    mag[j] = __float_as_uint(x[j]) & 0x7fffffffu;
+    if (mag[j] < 0x7f800000u) top = max(top, mag[j]); else wild |= 1u << j;
+  }
+#pragma unroll
+  for (int o = 1; o < kStateBlock / 4; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  byte = (uint32_t)max((int)((top + 0x200000u) >> 23) - 8, 0);
+  const float inverse = __uint_as_float((254u - byte) << 23);
+  uint32_t codes = 0u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float u = __uint_as_float(mag[j]) * inverse * 7.5231638e-37f;            // 2^-120
+    uint32_t c = (__float_as_uint(u) + (random[j] << 4)) >> 20;
+    if (above_zero && mag[j] != 0u) c = max(c, 1u);
+    if (wild >> j & 1u) c = 0x7fu;
+    codes |= (c | (__float_as_uint(x[j]) >> 31 << 7)) << (8 * j);
+  }
+  return codes;
+}
+
+__device__ __forceinline__ float root(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+
+template <int N, int BITS>
+__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamBatch<N> B) {
+  constexpr int kSize = BITS / 8;                                // bytes of a state
+  int lo = 0, hi = B.n - 1;                                      // the last tensor that starts at or before this chunk
+  while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (B.chunk0[mid] <= blockIdx.x) lo = mid; else hi = mid - 1; }
+  const AdamTensor& t = B.t[lo];
+  const AdamHyper& h = B.h;
+  const bool vec = t.vec != 0u;
+  const int64_t first = (int64_t)(blockIdx.x - B.chunk0[lo]) * kAdamChunk + threadIdx.x * 4;
+  const int psize = type_bytes(t.type), gsize = type_bytes(h.grad_type);
+  const bool has_master = t.master != nullptr;
+  uint4 rp[kAdamGroups], rg[kAdamGroups], rm[kAdamGroups], rv[kAdamGroups];
+  uint32_t bm[kAdamGroups], bv[kAdamGroups];
+#pragma unroll
+  for (int u = 0; u < kAdamGroups; ++u) {
+    const int64_t e = first + u * (kAdamThreads * 4);
+    const int count = (int)max((int64_t)0, min((int64_t)4, t.n - e));
+    rg[u] = load_raw4(t.g, gsize, e, count, vec);
+    rp[u] = has_master ? load_raw4(t.master, 4, e, count, vec) : load_raw4(t.p, psize, e, count, vec);
+    rm[u] = load_raw4(t.m, kSize, e, count, vec);
+    rv[u] = load_raw4(t.v, kSize, e, count, vec);
+    if constexpr (BITS == 8) {
+      bm[u] = count > 0 ? t.ms[e / kStateBlock] : 0u;
+      bv[u] = count > 0 ? t.vs[e / kStateBlock] : 0u;
+    }
+  }
+  const float c = h.scale ? h.scale[1] : 1.0f;
+  if (!(fabsf(c) <= 3.0e38f)) return;                             // the gradient's norm was not finite: nothing is updated
+  const float decay = -h.lr * t.decay;
+#pragma unroll
+  for (int u = 0; u < kAdamGroups; ++u) {
+    const int64_t e = first + u * (kAdamThreads * 4);
+    const int count = (int)max((int64_t)0, min((int64_t)4, t.n - e));
+    float p[4], g[4], m[4], v[4];
+    unpack4(rg[u], h.grad_type, g);
+    unpack4(rp[u], has_master ? ATOMO_TYPE_F32 : t.type, p);
+    if constexpr (BITS == 8) { state_decode(rm[u].x, bm[u], m); state_decode(rv[u].x, bv[u], v); }
+    else { unpack4(rm[u], ATOMO_TYPE_F32, m); unpack4(rv[u], ATOMO_TYPE_F32, v); }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      g[j] *= c;
+      m[j] = fmaf(h.beta1, m[j], h.one_minus_beta1 * g[j]);
+      v[j] = fmaf(h.beta2, v[j], h.one_minus_beta2 * g[j] * g[j]);
+      const float d = fmaf(root(v[j]), h.inv_root_bias2, h.eps);
+      p[j] = fmaf(-h.step_size, __fdividef(m[j], d), fmaf(decay, p[j], p[j]));
+    }
+    if constexpr (BITS == 8) {
+      const uint64_t block = (uint64_t)e >> 2;
+      const uint4 w = philox4x32_10(make_uint4((uint32_t)block, (uint32_t)(block >> 32) | 0x80000000u, t.index, h.step & 0x7fffffffu), h.key);
+      const uint32_t r0[4] = {w.x & 0xffffu, w.y & 0xffffu, w.z & 0xffffu, w.w & 0xffffu}, r1[4] = {w.x >> 16, w.y >> 16, w.z >> 16, w.w >> 16};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) if (j >= count) { m[j] = 0.0f; v[j] = 0.0f; }
+      uint32_t new_m, new_v;
+      const uint32_t cm = state_encode(m, r0, false, new_m), cv = state_encode(v, r1, true, new_v);
+      if (count > 0) {
+        store_raw4(t.m, 1, e, count, vec, make_uint4(cm, 0u, 0u, 0u));
+        store_raw4(t.v, 1, e, count, vec, make_uint4(cv, 0u, 0u, 0u));
+        if (e % kStateBlock == 0) { t.ms[e / kStateBlock] = (uint8_t)new_m; t.vs[e / kStateBlock] = (uint8_t)new_v; }
+      }
+    } else {
+      store_raw4(t.m, 4, e, count, vec, pack4(m, ATOMO_TYPE_F32));
+      store_raw4(t.v, 4, e, count, vec, pack4(v, ATOMO_TYPE_F32));
+    }
+    if (has_master) store_raw4(t.master, 4, e, count, vec, pack4(p, ATOMO_TYPE_F32));
+    store_raw4(t.p, psize, e, count, vec, pack4(p, t.type));
+  }
+}
+
+bool apart(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+template <int N>
+cudaError_t adamw_batch(const atomo_adamw_tensor* ts, const void* const* grads, const int* index, int n, int bits, const AdamHyper& h, cudaStream_t st) {
+  AdamBatch<N> B;
+  uint64_t at = 0;
+  const int ssize = bits / 8;
+  for (int i = 0; i < n; ++i) {
+    const atomo_adamw_tensor& t = ts[index[i]];
+    const void* g = grads[index[i]];
+    const bool vec = apart(t.param, 4 * type_bytes(t.type)) && apart(g, 4 * type_bytes(h.grad_type)) && apart(t.exp_avg, 4 * ssize) &&
+                     apart(t.exp_avg_sq, 4 * ssize) && apart(t.master, 16);
+    B.t[i] = AdamTensor{t.param, g, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale, t.master, t.n, t.weight_decay, t.type, (uint32_t)index[i], vec};
+    B.chunk0[i] = (uint32_t)at;
+    at += (uint64_t)((t.n + kAdamChunk - 1) / kAdamChunk);
+  }
+  B.n = n; B.h = h;
+  if (bits == 8) adamw_kernel<N, 8><<<(unsigned)at, kAdamThreads, 0, st>>>(B);
+  else adamw_kernel<N, 32><<<(unsigned)at, kAdamThreads, 0, st>>>(B);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+int launch_adamw(const atomo_adamw_tensor* tensors, const void* const* grads, int n, int bits, const AdamHyper& h, cudaStream_t st) {
+  constexpr int kMost = 380;                                     // 84 bytes each: just under 32 KB of kernel arguments
+  constexpr uint64_t kMostChunks = 0x7fffffffull;                // CTAs of a launch
+  std::vector<int> index;
+  index.reserve(n);
+  for (int i = 0; i < n; ++i) if (tensors[i].n > 0) index.push_back(i);
+  for (int i0 = 0; i0 < (int)index.size();) {
+    int count = 0;
+    uint64_t chunks = 0;
+    while (i0 + count < (int)index.size() && count < kMost) {
+      const uint64_t c = (uint64_t)((tensors[index[i0 + count]].n + kAdamChunk - 1) / kAdamChunk);
+      if (count > 0 && chunks + c > kMostChunks) break;
+      chunks += c; ++count;
+    }
+    const cudaError_t e = count <= 8 ? adamw_batch<8>(tensors, grads, &index[i0], count, bits, h, st)
+                        : count <= 64 ? adamw_batch<64>(tensors, grads, &index[i0], count, bits, h, st)
+                                      : adamw_batch<kMost>(tensors, grads, &index[i0], count, bits, h, st);
+    if (e != cudaSuccess) return (int)e;
+    i0 += count;
+  }
+  return (int)cudaSuccess;
+}
+
+}  // namespace atomo

@@ -1,0 +1,89 @@
+"""GPU: a training step from the tokens to the weights as it is used: embedding, layer norm and their gradients, both workers' gradients encoded,
+the payloads averaged, norm and clipping, AdamW."""
+import numpy as np
+import pytest
+import torch
+
+from tests import operator_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+ROWS, COLS, TOKENS = 120, 64, 500
+SCALE = COLS ** 0.5
+
+
+@pytest.fixture(scope="module")
+def atomo():
+    from paper_1806_04090_b200 import api
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    a = api.Atomo(0)
+    yield a
+    a.close()
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _backward(atomo, table, weight, bias, ids, target):
+    """Gradients of sum((layer_norm(embedding) - target)^2) / 2, in fp32."""
+    x = atomo.atomo_embedding(table, ids, scale=SCALE)
+    y, mean, rstd = atomo.atomo_layer_norm(x, weight, bias)
+    dx, dweight, dbias = atomo.atomo_layer_norm_backward(y - target, x, weight, mean, rstd)
+    return atomo.atomo_embedding_backward(ids, dx, ROWS, scale=SCALE), dweight, dbias
+
+
+@pytest.mark.parametrize("spectral", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_step(atomo, spectral, bits):
+    from paper_1806_04090_b200 import api
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(31)
+    table = torch.randn(ROWS, COLS, generator=gen, device="cuda") * 0.3
+    weight, bias = torch.ones(COLS, device="cuda"), torch.zeros(COLS, device="cuda")
+    params = [table, weight, bias]
+    old = [_np(p) for p in params]
+    state = api.AdamWState.zeros(params, bits=bits, weight_decay=[0.1, 0.0, 0.0])
+    payloads, small, wanted = [], [], []
+    for worker in range(2):
+        ids = torch.randint(0, ROWS, (TOKENS,), generator=gen, device="cuda")
+        target = torch.randn(TOKENS, COLS, generator=gen, device="cuda")
+        grads = _backward(atomo, table, weight, bias, ids, target)
+        # against autograd in 64 bits; the chain's roundings are below 1e-5 of the gradients' sizes (500 terms of about eight roundings each: 4e-6)
+        t, w, b = (p.double().requires_grad_(True) for p in params)
+        h = t[ids] * SCALE
+        h = (h - h.mean(1, keepdim=True)) / (h.var(1, keepdim=True, correction=0) + 1e-5).sqrt() * w + b
+        exact = torch.autograd.grad(((h - target) ** 2).sum() / 2, (t, w, b))
+        for g, e in zip(grads, exact):
+            assert float((g.double() - e).abs().max()) <= 1e-5 * float(e.abs().max())
+        # the table is encoded; a budget that keeps every atom makes the payload's decode the gradient
+        if spectral:
+            pay, _ = atomo.atomo_encode_spectral([grads[0]], float(COLS), seed=worker, step=1, k_cap=COLS)
+        else:
+            pay, _ = atomo.atomo_encode_entrywise([grads[0].view(-1)], float(ROWS * COLS), seed=worker, step=1, k_cap=ROWS * COLS)
+        payloads.append(pay)
+        small.append(grads[1:])
+        wanted.append([_np(e) for e in exact])
+    mean = [atomo.atomo_decode_average(payloads)[0]] + [(a + b) / 2 for a, b in zip(*small)]
+    for m, a, b in zip(mean, *wanted):
+        want = (a + b) / 2
+        assert np.abs(_np(m).reshape(want.shape) - want).max() <= (2e-3 if spectral else 1e-5) * np.abs(want).max()   # spectral: vectors of an fp32 Gram matrix
+    scale = atomo.atomo_grad_norm(mean, max_norm=1.0)
+    norm = np.sqrt(sum((_np(m) ** 2).sum() for m in mean))
+    assert norm > 1.0 and abs(float(scale[0]) / norm - 1) <= 18 * ref.U32 and abs(float(scale[1]) * (norm + 1e-6) - 1) <= 20 * ref.U32
+    atomo.atomo_adamw(state, mean, lr=1e-2, step=1, seed=9, scale=scale)
+    for p, g, before, decay in zip(params, mean, old, state.weight_decay):
+        (want, _, _), (off, _, _) = ref.adamw(before.reshape(-1), _np(g).reshape(-1), np.zeros(g.numel()), np.zeros(g.numel()), 1e-2, 1, 0.9, 0.999, 1e-8, decay, float(scale[1]))
+        ref.near(p, want.reshape(p.shape), off.reshape(p.shape))
+
+
+def test_a_sparse_table_gradient_keeps_its_zero_rows_through_the_exchange(atomo):
+    """Rows without tokens are exact zeros, so no atom of theirs is ever kept."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(32)
+    ids = torch.randint(0, ROWS // 4, (TOKENS,), generator=gen, device="cuda") * 4
+    grad = atomo.atomo_embedding_backward(ids, torch.randn(TOKENS, COLS, generator=gen, device="cuda"), ROWS)
+    for s in (50.0, 1000.0):
+        pay, _ = atomo.atomo_encode_entrywise([grad.view(-1)], s, seed=3, step=2)
+        out = atomo.atomo_decode(pay)[0].view(ROWS, COLS)
+        assert atomo.payload_status(pay)[0] == 0 and bool((out[grad == 0] == 0).all()) and int((out != 0).sum()) > 0
