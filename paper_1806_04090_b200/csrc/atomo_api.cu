@@ -1535,7 +1535,7 @@ int atomo_adamw(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, const void* c
   h.step_size = (float)(a.lr / (1.0 - std::pow(a.beta1, (double)a.step)));
   h.inv_root_bias2 = (float)(1.0 / std::sqrt(1.0 - std::pow(a.beta2, (double)a.step)));
   h.scale = a.scale; h.step = (uint32_t)a.step; h.grad_type = a.grad_type;
-  h.key = PhiloxKey{(uint32_t)a.seed, (uint32_t)(a.seed >> 32)};
+  h.key = philox_round_keys(PhiloxKey{(uint32_t)a.seed, (uint32_t)(a.seed >> 32)});
   return on_device(ctx, "adamw", [&] { return launch_adamw(tensors, grads, n_tensors, a.state_bits, h, (cudaStream_t)stream); });
 }
 

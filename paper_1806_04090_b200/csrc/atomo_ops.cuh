@@ -53,7 +53,7 @@ struct AdamHyper {
   float lr, step_size, inv_root_bias2, eps;   // step_size = lr / (1 - beta1^t), inv_root_bias2 = 1 / sqrt(1 - beta2^t)
   const float* scale;                         // DEVICE: {norm, factor of the gradient}, or null
   uint32_t step; int32_t grad_type;
-  PhiloxKey key;
+  PhiloxRoundKeys key;
 };
 int launch_adamw(const atomo_adamw_tensor* tensors, const void* const* grads, int n, int bits, const AdamHyper& h, cudaStream_t st);   // cudaError_t
 

@@ -218,14 +218,15 @@ namespace {
 
 // =================================== AdamW =======================================================
 // m = b1 m + (1 - b1) c g,  v = b2 v + (1 - b2) (c g)^2,  p = p - lr wd p - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps),
-// all in fp32; c is read from device memory.  A thread takes four neighbouring elements kAdamGroups times, all loads first.
-constexpr int kAdamThreads = 256, kAdamGroups = 4;
-constexpr int kAdamChunk = kAdamThreads * 4 * kAdamGroups;
+// all in fp32; c is read from device memory.  A CTA takes kAdamChunk neighbouring elements of a tensor, a thread several groups of
+// neighbouring ones, all loads first.  Chunks that lie inside an aligned tensor go through adam_inside, compiled for the types (with 8-bit states
+// instruction issue bounds the kernel as much as memory does); a tensor's last chunk, and tensors of other alignment, through adam_any.
+constexpr int kAdamThreads = 256, kAdamChunk = 2048;
 constexpr int kStateBlock = ATOMO_STATE_BLOCK;
 
 struct AdamTensor {
   void* p; const void* g; void* m; void* v; uint8_t* ms; uint8_t* vs; float* master;
-  int64_t n; float decay; int32_t type; uint32_t index, vec;     // vec: every array may be moved four elements at a time
+  int64_t n; float decay; int32_t type; uint32_t index, vec;     // vec: every array may be moved in whole groups
 };
 template <int N> struct AdamBatch {
   AdamTensor t[N];
@@ -233,6 +234,115 @@ template <int N> struct AdamBatch {
   int n; AdamHyper h;
 };
 
+__device__ __forceinline__ float root(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+
+__device__ __forceinline__ void adam_element(const AdamHyper& h, float c, float decay, float g, float& p, float& m, float& v) {
+  g *= c;
+  m = fmaf(h.beta1, m, h.one_minus_beta1 * g);
+  v = fmaf(h.beta2, v, h.one_minus_beta2 * g * g);
+  const float d = fmaf(root(v), h.inv_root_bias2, h.eps);
+  p = fmaf(-h.step_size, __fdividef(m, d), fmaf(decay, p, p));
+}
+
+// The same for pairs of elements, on packed fp32, without the care for subnormal numbers that root and quotient take: a second moment below 2^-126
+// counts as zero, which is nothing beside an eps of kEpsPairs (1e-19 in 1e-12); smaller ones go through adam_element.
+constexpr float kEpsPairs = 1.0e-12f;
+struct AdamPairs { uint64_t c, b1, r1, b2, r2, inv, eps, decay, step; };
+__device__ __forceinline__ AdamPairs adam_pairs(const AdamHyper& h, float c, float decay) {
+  auto both = [](float x) { return pack2(x, x); };
+  return AdamPairs{both(c), both(h.beta1), both(h.one_minus_beta1), both(h.beta2), both(h.one_minus_beta2), both(h.inv_root_bias2), both(h.eps), both(decay), both(-h.step_size)};
+}
+__device__ __forceinline__ void adam_pair(const AdamPairs& k, const float* g, float* p, float* m, float* v) {
+  const uint64_t g2 = mul2(pack2(g[0], g[1]), k.c), p2 = pack2(p[0], p[1]);
+  const uint64_t m2 = fma2(k.b1, pack2(m[0], m[1]), mul2(k.r1, g2));
+  const uint64_t v2 = fma2(mul2(k.r2, g2), g2, mul2(k.b2, pack2(v[0], v[1])));
+  unpack2(m2, m[0], m[1]); unpack2(v2, v[0], v[1]);
+  float s0, s1;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(s0) : "f"(v[0]));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(s1) : "f"(v[1]));
+  unpack2(fma2(pack2(s0, s1), k.inv, k.eps), s0, s1);
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(s0));
+  asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(s1));
+  unpack2(fma2(k.step, mul2(m2, pack2(s0, s1)), fma2(k.decay, p2, p2)), p[0], p[1]);
+}
+
+// ---- states in 8 bits: e4m3 codes times a power of two for each 32 neighbouring elements, kept as its exponent byte ----
+__device__ __forceinline__ float state_scale(uint32_t byte) { return __uint_as_float(byte > 0u ? byte << 23 : 0x00400000u); }
+__device__ __forceinline__ void state_decode(uint32_t codes, float s, float* x) {
+  uint32_t lo, hi;
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(codes));
+  const float2 a = __half22float2(*reinterpret_cast<__half2*>(&lo)), b = __half22float2(*reinterpret_cast<__half2*>(&hi));
+  const uint64_t s2 = pack2(s, s);
+  unpack2(mul2(pack2(a.x, a.y), s2), x[0], x[1]); unpack2(mul2(pack2(b.x, b.y), s2), x[2], x[3]);
+}
+// The power of two brings the block's largest finite magnitude into [224, 448), so that rounding it up stays within e4m3.  The magnitude
+// times 2^-120 has e4m3's exponent in the exponent field of fp32, subnormal numbers included, so that its code is bits 27 to 20;
+// 16 random bits added below them round up with the probability of what is cut off (to 2^-16 of a step).  All of it four bits
+// further up leaves the code in the top byte.
+// ABOVE_ZERO: a value above zero is never rounded to zero (a second moment of zero beside a first moment that is not would make a
+// step of any size).  What is not finite becomes NaN.
+// PER neighbouring elements per thread; the high (HIGH) or low 16 bits of their random words.
+template <int PER, bool ABOVE_ZERO, bool HIGH>
+__device__ __forceinline__ void state_encode(const float (&x)[PER], const uint32_t (&random)[PER], uint32_t (&codes)[PER / 4], uint32_t& byte) {
+  constexpr uint32_t kMask = ABOVE_ZERO ? 0xffffffffu : 0x7fffffffu;          // (a second moment has no sign)
+  float y[PER], factor;
+  uint32_t top = 0u;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) { y[j] = __uint_as_float(__float_as_uint(x[j]) & kMask); top = max(top, __float_as_uint(y[j])); }
+#pragma unroll
+  for (int o = 1; o < kStateBlock / PER; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  // up to here one factor does (an exponent byte of at most 133): beyond, values of 2^14 and more, and those that are not finite
+  const bool plain = __all_sync(0xffffffffu, top < 0x46e00000u);
+  if (plain) {
+    byte = (uint32_t)max((int)((top + 0x200000u) >> 23) - 8, 0);
+    factor = __uint_as_float((134u - byte) << 23);
+  } else {
+    top = 0u;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) { const uint32_t a = __float_as_uint(y[j]); if (a < 0x7f800000u) top = max(top, a); }
+#pragma unroll
+    for (int o = 1; o < kStateBlock / PER; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    byte = (uint32_t)max((int)((top + 0x200000u) >> 23) - 8, 0);
+    factor = __uint_as_float(7u << 23);                          // 2^-120
+#pragma unroll
+    for (int j = 0; j < PER; ++j) y[j] *= __uint_as_float((254u - byte) << 23);
+  }
+  // (The product is written as a packed one: with a scalar one the compiler's results were zero here, as tests/test_gpu_step.py shows.)
+  uint32_t t[PER], least = 0xffffffffu;
+  const uint64_t factors = pack2(factor, factor);
+#pragma unroll
+  for (int j = 0; j < PER; j += 2) {
+    float a, b;
+    unpack2(mul2(pack2(y[j], y[j + 1]), factors), a, b);
+    t[j] = __float_as_uint(a) * 16u + __byte_perm(random[j], 0u, HIGH ? 0x4324 : 0x4104);                  // the 16 bits in bytes 1 and 2
+    t[j + 1] = __float_as_uint(b) * 16u + __byte_perm(random[j + 1], 0u, HIGH ? 0x4324 : 0x4104);
+    least = min(least, min(t[j], t[j + 1]));
+  }
+  if (!plain) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) if ((__float_as_uint(x[j]) & 0x7fffffffu) >= 0x7f800000u) t[j] = 0x7f000000u;
+  }
+  if (ABOVE_ZERO && least < 1u << 24) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) t[j] = x[j] > 0.0f ? max(t[j], 1u << 24) : t[j];
+  }
+#pragma unroll
+  for (int q = 0; q < PER / 4; ++q) {
+    const uint32_t a = __byte_perm(t[4 * q], t[4 * q + 1], 0x0073), b = __byte_perm(t[4 * q + 2], t[4 * q + 3], 0x0073);
+    codes[q] = __byte_perm(a, b, 0x5410);
+    if (!ABOVE_ZERO) {                                           // signs
+      const uint32_t sa = __byte_perm(__float_as_uint(x[4 * q]), __float_as_uint(x[4 * q + 1]), 0x0073);
+      const uint32_t sb = __byte_perm(__float_as_uint(x[4 * q + 2]), __float_as_uint(x[4 * q + 3]), 0x0073);
+      codes[q] |= __byte_perm(sa, sb, 0x5410) & 0x80808080u;
+    }
+  }
+}
+__device__ __forceinline__ uint4 state_words(const AdamHyper& h, uint32_t tensor, int64_t e) {
+  const uint64_t block = (uint64_t)e >> 2;
+  return philox4x32_10(make_uint4((uint32_t)block, (uint32_t)(block >> 32) | 0x80000000u, tensor, h.step & 0x7fffffffu), h.key);
+}
+
+// ---- any alignment and any types, four elements at a time ----
 // four elements of `size` bytes each as they lie in memory, in the low words of r; `count` of them exist
 __device__ __forceinline__ uint4 load_raw4(const void* base, int size, int64_t e, int count, bool vec) {
   uint4 r = make_uint4(0u, 0u, 0u, 0u);
@@ -296,102 +406,39 @@ __device__ __forceinline__ uint4 pack4(const float (&x)[4], int type) {
   return r;
 }
 
-// A state in 8 bits: e4m3 codes times a power of two for each 32 neighbouring elements, kept as its exponent byte.
-__device__ __forceinline__ float state_scale(uint32_t byte) { return __uint_as_float(byte > 0u ? byte << 23 : 0x00400000u); }
-__device__ __forceinline__ void state_decode(uint32_t codes, uint32_t byte, float (&x)[4]) {
-  uint32_t lo, hi;
-  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(codes));
-  const float s = state_scale(byte);
-  const float2 a = __half22float2(*reinterpret_cast<__half2*>(&lo)), b = __half22float2(*reinterpret_cast<__half2*>(&hi));
-  x[0] = a.x * s; x[1] = a.y * s; x[2] = b.x * s; x[3] = b.y * s;
-}
-// The power of two brings the block's largest finite magnitude into [224, 448), so that rounding it up stays within e4m3.  The magnitude
-// times 2^-120 has e4m3's exponent in the exponent field of fp32, subnormal numbers included, so that its code is the upper 12 of
-// the 32 bits; 16 random bits added below them round up with the probability of what is cut off (to 2^-16 of a step).
-// above_zero: a value above zero is never rounded to zero (a second moment of zero beside a first moment that is not would make a
-// step of any size).  What is not finite becomes NaN.
-__device__ __forceinline__ uint32_t state_encode(const float (&x)[4], const uint32_t (&random)[4], bool above_zero, uint32_t& byte) {
-  uint32_t mag[4], top = 0u, wild = 0u;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    mag[j] = __float_as_uint(x[j]) & 0x7fffffffu;
-    if (mag[j] < 0x7f800000u) top = max(top, mag[j]); else wild |= 1u << j;
-  }
-#pragma unroll
-  for (int o = 1; o < kStateBlock / 4; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  byte = (uint32_t)max((int)((top + 0x200000u) >> 23) - 8, 0);
-  const float inverse = __uint_as_float((254u - byte) << 23);
-  uint32_t codes = 0u;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float u = __uint_as_float(mag[j]) * inverse * 7.5231638e-37f;            // 2^-120
-    uint32_t c = (__float_as_uint(u) + (random[j] << 4)) >> 20;
-    if (above_zero && mag[j] != 0u) c = max(c, 1u);
-    if (wild >> j & 1u) c = 0x7fu;
-    codes |= (c | (__float_as_uint(x[j]) >> 31 << 7)) << (8 * j);
-  }
-  return codes;
-}
-
-__device__ __forceinline__ float root(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-
-template <int N, int BITS>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamBatch<N> B) {
+template <int BITS>
+__device__ __noinline__ void adam_any(const AdamTensor& t, const AdamHyper& h, int64_t first, float c) {
   constexpr int kSize = BITS / 8;                                // bytes of a state
-  int lo = 0, hi = B.n - 1;                                      // the last tensor that starts at or before this chunk
-  while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (B.chunk0[mid] <= blockIdx.x) lo = mid; else hi = mid - 1; }
-  const AdamTensor& t = B.t[lo];
-  const AdamHyper& h = B.h;
-  const bool vec = t.vec != 0u;
-  const int64_t first = (int64_t)(blockIdx.x - B.chunk0[lo]) * kAdamChunk + threadIdx.x * 4;
-  const int psize = type_bytes(t.type), gsize = type_bytes(h.grad_type);
-  const bool has_master = t.master != nullptr;
-  uint4 rp[kAdamGroups], rg[kAdamGroups], rm[kAdamGroups], rv[kAdamGroups];
-  uint32_t bm[kAdamGroups], bv[kAdamGroups];
-#pragma unroll
-  for (int u = 0; u < kAdamGroups; ++u) {
-    const int64_t e = first + u * (kAdamThreads * 4);
-    const int count = (int)max((int64_t)0, min((int64_t)4, t.n - e));
-    rg[u] = load_raw4(t.g, gsize, e, count, vec);
-    rp[u] = has_master ? load_raw4(t.master, 4, e, count, vec) : load_raw4(t.p, psize, e, count, vec);
-    rm[u] = load_raw4(t.m, kSize, e, count, vec);
-    rv[u] = load_raw4(t.v, kSize, e, count, vec);
-    if constexpr (BITS == 8) {
-      bm[u] = count > 0 ? t.ms[e / kStateBlock] : 0u;
-      bv[u] = count > 0 ? t.vs[e / kStateBlock] : 0u;
-    }
-  }
-  const float c = h.scale ? h.scale[1] : 1.0f;
-  if (!(fabsf(c) <= 3.0e38f)) return;                             // the gradient's norm was not finite: nothing is updated
+  const bool vec = t.vec != 0u, has_master = t.master != nullptr;
+  const int psize = type_bytes(t.type);
   const float decay = -h.lr * t.decay;
-#pragma unroll
-  for (int u = 0; u < kAdamGroups; ++u) {
-    const int64_t e = first + u * (kAdamThreads * 4);
+#pragma unroll 2
+  for (int u = 0; u < kAdamChunk / (kAdamThreads * 4); ++u) {
+    const int64_t e = first + (u * kAdamThreads + threadIdx.x) * 4;
     const int count = (int)max((int64_t)0, min((int64_t)4, t.n - e));
+    const uint4 rg = load_raw4(t.g, type_bytes(h.grad_type), e, count, vec);
+    const uint4 rp = has_master ? load_raw4(t.master, 4, e, count, vec) : load_raw4(t.p, psize, e, count, vec);
+    const uint4 rm = load_raw4(t.m, kSize, e, count, vec), rv = load_raw4(t.v, kSize, e, count, vec);
     float p[4], g[4], m[4], v[4];
-    unpack4(rg[u], h.grad_type, g);
-    unpack4(rp[u], has_master ? ATOMO_TYPE_F32 : t.type, p);
-    if constexpr (BITS == 8) { state_decode(rm[u].x, bm[u], m); state_decode(rv[u].x, bv[u], v); }
-    else { unpack4(rm[u], ATOMO_TYPE_F32, m); unpack4(rv[u], ATOMO_TYPE_F32, v); }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      g[j] *= c;
-      m[j] = fmaf(h.beta1, m[j], h.one_minus_beta1 * g[j]);
-      v[j] = fmaf(h.beta2, v[j], h.one_minus_beta2 * g[j] * g[j]);
-      const float d = fmaf(root(v[j]), h.inv_root_bias2, h.eps);
-      p[j] = fmaf(-h.step_size, __fdividef(m[j], d), fmaf(decay, p[j], p[j]));
-    }
+    unpack4(rg, h.grad_type, g);
+    unpack4(rp, has_master ? (int)ATOMO_TYPE_F32 : t.type, p);
     if constexpr (BITS == 8) {
-      const uint64_t block = (uint64_t)e >> 2;
-      const uint4 w = philox4x32_10(make_uint4((uint32_t)block, (uint32_t)(block >> 32) | 0x80000000u, t.index, h.step & 0x7fffffffu), h.key);
-      const uint32_t r0[4] = {w.x & 0xffffu, w.y & 0xffffu, w.z & 0xffffu, w.w & 0xffffu}, r1[4] = {w.x >> 16, w.y >> 16, w.z >> 16, w.w >> 16};
+      const uint32_t bm = count > 0 ? t.ms[e / kStateBlock] : 0u, bv = count > 0 ? t.vs[e / kStateBlock] : 0u;
+      state_decode(rm.x, state_scale(bm), m); state_decode(rv.x, state_scale(bv), v);
+    } else { unpack4(rm, ATOMO_TYPE_F32, m); unpack4(rv, ATOMO_TYPE_F32, v); }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) adam_element(h, c, decay, g[j], p[j], m[j], v[j]);
+    if constexpr (BITS == 8) {
+      const uint4 w = state_words(h, t.index, e);
+      const uint32_t random[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) if (j >= count) { m[j] = 0.0f; v[j] = 0.0f; }
-      uint32_t new_m, new_v;
-      const uint32_t cm = state_encode(m, r0, false, new_m), cv = state_encode(v, r1, true, new_v);
+      uint32_t new_m, new_v, cm[1], cv[1];
+      state_encode<4, false, false>(m, random, cm, new_m);
+      state_encode<4, true, true>(v, random, cv, new_v);
       if (count > 0) {
-        store_raw4(t.m, 1, e, count, vec, make_uint4(cm, 0u, 0u, 0u));
-        store_raw4(t.v, 1, e, count, vec, make_uint4(cv, 0u, 0u, 0u));
+        store_raw4(t.m, 1, e, count, vec, make_uint4(cm[0], 0u, 0u, 0u));
+        store_raw4(t.v, 1, e, count, vec, make_uint4(cv[0], 0u, 0u, 0u));
         if (e % kStateBlock == 0) { t.ms[e / kStateBlock] = (uint8_t)new_m; t.vs[e / kStateBlock] = (uint8_t)new_v; }
       }
     } else {
@@ -401,6 +448,128 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
     if (has_master) store_raw4(t.master, 4, e, count, vec, pack4(p, ATOMO_TYPE_F32));
     store_raw4(t.p, psize, e, count, vec, pack4(p, t.type));
   }
+}
+
+// ---- a chunk inside an aligned tensor ----
+template <typename T, int PER> __device__ __forceinline__ void load_group(const T* p, float (&x)[PER]) {
+  constexpr int kVec = 16 / (int)sizeof(T) < PER ? 16 / (int)sizeof(T) : PER;
+#pragma unroll
+  for (int k = 0; k < PER; k += kVec) {
+    const Pack<T, kVec> r = load_pack<T, kVec>(p + k);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) x[k + j] = to_float(r.v[j]);
+  }
+}
+template <typename T, int PER> __device__ __forceinline__ void store_group(T* p, const float (&x)[PER]) {
+  constexpr int kVec = 16 / (int)sizeof(T) < PER ? 16 / (int)sizeof(T) : PER;
+#pragma unroll
+  for (int k = 0; k < PER; k += kVec) {
+    Pack<T, kVec> r;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) r.v[j] = from_float<T>(x[k + j]);
+    store_pack<T, kVec>(p + k, r);
+  }
+}
+
+// Elements per group: with 8-bit states eight, so that four lanes share a block.
+template <int BITS, typename P, typename G, bool MASTER>
+__device__ __forceinline__ void adam_inside(const AdamTensor& t, const AdamHyper& h, int64_t first, float c) {
+  constexpr int PER = BITS == 8 ? 8 : 4, kGroups = kAdamChunk / (kAdamThreads * PER);
+  const AdamPairs k = adam_pairs(h, c, -h.lr * t.decay);
+  P* tp = static_cast<P*>(t.p) + first + threadIdx.x * PER;
+  float* tw = t.master + first + threadIdx.x * PER;
+  const G* tg = static_cast<const G*>(t.g) + first + threadIdx.x * PER;
+  float p[kGroups][PER], g[kGroups][PER];
+  if constexpr (BITS == 32) {
+    float* tm = static_cast<float*>(t.m) + first + threadIdx.x * PER;
+    float* tv = static_cast<float*>(t.v) + first + threadIdx.x * PER;
+    float m[kGroups][PER], v[kGroups][PER];
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) {
+      constexpr int kStep = kAdamThreads * PER;
+      load_group<G, PER>(tg + u * kStep, g[u]);
+      if constexpr (MASTER) load_group<float, PER>(tw + u * kStep, p[u]); else load_group<P, PER>(tp + u * kStep, p[u]);
+      load_group<float, PER>(tm + u * kStep, m[u]);
+      load_group<float, PER>(tv + u * kStep, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) {
+      constexpr int kStep = kAdamThreads * PER;
+#pragma unroll
+      for (int j = 0; j < PER; j += 2) adam_pair(k, g[u] + j, p[u] + j, m[u] + j, v[u] + j);
+      store_group<float, PER>(tm + u * kStep, m[u]);
+      store_group<float, PER>(tv + u * kStep, v[u]);
+      if constexpr (MASTER) store_group<float, PER>(tw + u * kStep, p[u]);
+      store_group<P, PER>(tp + u * kStep, p[u]);
+    }
+  } else {
+    uint8_t* tm = static_cast<uint8_t*>(t.m) + first + threadIdx.x * PER;
+    uint8_t* tv = static_cast<uint8_t*>(t.v) + first + threadIdx.x * PER;
+    uint8_t* sm = t.ms + first / kStateBlock + threadIdx.x * PER / kStateBlock;
+    uint8_t* sv = t.vs + first / kStateBlock + threadIdx.x * PER / kStateBlock;
+    uint2 rm[kGroups], rv[kGroups];
+    uint32_t bm[kGroups], bv[kGroups];
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) {
+      constexpr int kStep = kAdamThreads * PER;
+      rm[u] = *reinterpret_cast<const uint2*>(tm + u * kStep); rv[u] = *reinterpret_cast<const uint2*>(tv + u * kStep);
+      bm[u] = sm[u * kStep / kStateBlock]; bv[u] = sv[u * kStep / kStateBlock];
+      load_group<G, PER>(tg + u * kStep, g[u]);
+      if constexpr (MASTER) load_group<float, PER>(tw + u * kStep, p[u]); else load_group<P, PER>(tp + u * kStep, p[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kGroups; ++u) {
+      constexpr int kStep = kAdamThreads * PER;
+      float m[PER], v[PER];
+      const float fm = state_scale(bm[u]), fv = state_scale(bv[u]);
+      state_decode(rm[u].x, fm, m); state_decode(rm[u].y, fm, m + 4);
+      state_decode(rv[u].x, fv, v); state_decode(rv[u].y, fv, v + 4);
+#pragma unroll
+      for (int j = 0; j < PER; j += 2) adam_pair(k, g[u] + j, p[u] + j, m + j, v + j);
+      if constexpr (MASTER) store_group<float, PER>(tw + u * kStep, p[u]);
+      store_group<P, PER>(tp + u * kStep, p[u]);
+      const int64_t e = first + (u * kAdamThreads + threadIdx.x) * PER;
+      const uint4 w0 = state_words(h, t.index, e), w1 = state_words(h, t.index, e + 4);
+      const uint32_t random[PER] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+      uint32_t new_m, new_v, cm[2], cv[2];
+      state_encode<PER, false, false>(m, random, cm, new_m);
+      state_encode<PER, true, true>(v, random, cv, new_v);
+      *reinterpret_cast<uint2*>(tm + u * kStep) = make_uint2(cm[0], cm[1]);
+      *reinterpret_cast<uint2*>(tv + u * kStep) = make_uint2(cv[0], cv[1]);
+      if (threadIdx.x % (kStateBlock / PER) == 0) { sm[u * kStep / kStateBlock] = (uint8_t)new_m; sv[u * kStep / kStateBlock] = (uint8_t)new_v; }
+    }
+  }
+}
+
+// Chunks of 2048 elements and five CTAs per SM, us (8-bit states, 25.6M elements | fp32 states, 11M | fp32 states and master copy, 133M): 77 | 51 | 550;
+// of 4096 and three per SM: 78 | 53 | 553; of 4096 and four: 90 | 53 | 562; of 2048 and six: 83 | 51 | 553.  The update by pairs took the instructions per
+// element with 8-bit states from 65 to 45 and the time from 82 to 77: memory bounds all three (413, 308 and 3738 MB).
+template <int N, int BITS>
+__global__ void __launch_bounds__(kAdamThreads, 5) adamw_kernel(const __grid_constant__ AdamBatch<N> B) {
+  int lo = 0, hi = B.n - 1;                                      // the last tensor that starts at or before this chunk
+  while (lo < hi) { const int mid = (lo + hi + 1) >> 1; if (B.chunk0[mid] <= blockIdx.x) lo = mid; else hi = mid - 1; }
+  const AdamTensor& t = B.t[lo];
+  const AdamHyper& h = B.h;
+  const int64_t first = (int64_t)(blockIdx.x - B.chunk0[lo]) * kAdamChunk;
+  const float c = h.scale ? h.scale[1] : 1.0f;
+  if (!(fabsf(c) <= 3.0e38f)) return;                             // the gradient's norm was not finite: nothing is updated
+  if (t.vec && first + kAdamChunk <= t.n && h.eps >= kEpsPairs) {
+    const bool same = h.grad_type == t.type, wide = h.grad_type == ATOMO_TYPE_F32, master = t.master != nullptr;
+    if (t.type == ATOMO_TYPE_F32) {
+      if (!master && wide) return adam_inside<BITS, float, float, false>(t, h, first, c);
+    } else if (t.type == ATOMO_TYPE_BF16) {
+      if (master && wide) return adam_inside<BITS, __nv_bfloat16, float, true>(t, h, first, c);
+      if (master && same) return adam_inside<BITS, __nv_bfloat16, __nv_bfloat16, true>(t, h, first, c);
+      if (!master && wide) return adam_inside<BITS, __nv_bfloat16, float, false>(t, h, first, c);
+      if (!master && same) return adam_inside<BITS, __nv_bfloat16, __nv_bfloat16, false>(t, h, first, c);
+    } else {
+      if (master && wide) return adam_inside<BITS, __half, float, true>(t, h, first, c);
+      if (master && same) return adam_inside<BITS, __half, __half, true>(t, h, first, c);
+      if (!master && wide) return adam_inside<BITS, __half, float, false>(t, h, first, c);
+      if (!master && same) return adam_inside<BITS, __half, __half, false>(t, h, first, c);
+    }
+  }
+  adam_any<BITS>(t, h, first, c);
 }
 
 bool apart(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
@@ -413,8 +582,7 @@ cudaError_t adamw_batch(const atomo_adamw_tensor* ts, const void* const* grads, 
   for (int i = 0; i < n; ++i) {
     const atomo_adamw_tensor& t = ts[index[i]];
     const void* g = grads[index[i]];
-    const bool vec = apart(t.param, 4 * type_bytes(t.type)) && apart(g, 4 * type_bytes(h.grad_type)) && apart(t.exp_avg, 4 * ssize) &&
-                     apart(t.exp_avg_sq, 4 * ssize) && apart(t.master, 16);
+    const bool vec = apart(t.param, 16) && apart(g, 16) && apart(t.exp_avg, ssize == 1 ? 8 : 16) && apart(t.exp_avg_sq, ssize == 1 ? 8 : 16) && apart(t.master, 16);
     B.t[i] = AdamTensor{t.param, g, t.exp_avg, t.exp_avg_sq, t.exp_avg_scale, t.exp_avg_sq_scale, t.master, t.n, t.weight_decay, t.type, (uint32_t)index[i], vec};
     B.chunk0[i] = (uint32_t)at;
     at += (uint64_t)((t.n + kAdamChunk - 1) / kAdamChunk);
