@@ -405,6 +405,7 @@ int atomo_create(atomo_ctx** out, int device) {
     for (int i = 0; i < ATOMO_N_STAGES; ++i) { CK(cudaEventCreate(&ctx->ev[r][i][0])); CK(cudaEventCreate(&ctx->ev[r][i][1])); }
   int e = sp_configure();
   if (e == 0) e = ew_configure();
+  if (e == 0) e = embedding_configure(device);
   if (e != 0) return fail_cuda(ctx, (cudaError_t)e, "cudaFuncSetAttribute(max dynamic shared memory)");
   ctx->tc_ok = sp_tc_configure() == 0;
   CK(cudaEventCreateWithFlags(&ctx->ev_fork, cudaEventDisableTiming));
@@ -1550,7 +1551,7 @@ int atomo_embedding(atomo_ctx* ctx, const void* table, int32_t type, int64_t row
 
 int64_t atomo_embedding_workspace_bytes(int64_t n_ids, int64_t rows, int64_t cols) {
   if (rows <= 0 || bad_shape(rows, cols, cols) || n_ids < 0 || n_ids > kMostRows) return -1;
-  return (int64_t)embedding_workspace(n_ids, rows, cols);
+  return (int64_t)embedding_workspace(n_ids, cols);
 }
 
 int atomo_embedding_backward(atomo_ctx* ctx, const void* ids, int32_t id_bytes, int64_t n_ids, const void* grad, int32_t type, int64_t ld, int64_t rows, int64_t cols,

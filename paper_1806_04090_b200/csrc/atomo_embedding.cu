@@ -5,10 +5,11 @@
 // The gradient's sums run in the order of the tokens, so that the same call gives the same bits each time (a payload that is encoded
 // from it does too), which sums by atomics would not.  Three kernels:
 //   emb_sort_kernel   stable radix sort of (id, token), eight bits a pass, by the CTAs of one cluster: they exchange their histograms
-//                     through distributed shared memory and their items through L2, with the hardware cluster barrier between.  It also
-//                     marks the rows that have tokens and lists the runs of equal ids that go over the end of a chunk.
-//   emb_sum_kernel    chunks of kEmbChunk neighbouring sorted tokens, so that a frequent token's run is split among CTAs: the sum of a run that lies
-//                     within a chunk goes to its row, the parts of longer ones to the workspace; other CTAs write the rows without tokens.
+//                     through distributed shared memory and their items through L2, with the hardware cluster barrier between; a tile's items are put in
+//                     order in shared memory first, so that they leave in runs.  It also lists the long runs of equal ids.  Meanwhile the launch's other CTAs write the rows
+//                     without tokens: each looks through the ids for those of its own rows, so that none of them waits for the sort.
+//   emb_sum_kernel    chunks of kEmbChunk neighbouring sorted tokens, so that a frequent token's run is split among CTAs.  A run that ends in the chunk it
+//                     starts in, or in the next one, is summed by the former and goes to its row; a longer one leaves one part per chunk in the workspace.
 //   emb_join_kernel   adds the parts of the longer runs, in order.
 // What bounds it is memory: dout is read once, the table's gradient written once.
 #include <algorithm>
@@ -20,7 +21,7 @@ namespace {
 
 constexpr int kEmbThreads = 256;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortItems = 8, kSortTile = kSortThreads * kSortItems;
-constexpr int kSortCluster = 8;
+constexpr int kSortClusterMax = 16;
 
 struct Ids { const void* p; int wide; };                         // wide: 64-bit
 __device__ __forceinline__ int64_t load_id(const Ids& ids, int64_t t) {
@@ -34,7 +35,7 @@ EmbShape emb_shape(int64_t cols, int vec) {
   const int64_t packs = (cols + vec - 1) / vec;
   EmbShape s;
   if (packs <= kEmbThreads / 2) {
-    s.cx = 4;                                                    // at most 64 rows, whose chunks' entries take 16 KB of shared memory
+    s.cx = 8;                                                    // at most 32 rows, whose chunks' items take 25 KB of shared memory
     while (s.cx < packs) s.cx <<= 1;
     s.cy = kEmbThreads / s.cx; s.slabs = 1;
   } else {
@@ -45,44 +46,54 @@ EmbShape emb_shape(int64_t cols, int vec) {
 }
 
 // ---- lookup ---------------------------------------------------------------------------------------
+// A CTA goes on to other tokens, whose ids it fetches while the rows are under way; what it writes is not kept in L2 for long, so that the rows of frequent
+// tokens stay.  64k tokens of 2048 bf16, us, CTAs per SM x tokens at a time: 6 x 2 60, 5 x 2 62, 6 x 1 64, 4 x 3 66, 4 x 4 66, 4 x 2 68, 3 x 4 70, 7 x 2 and
+// 8 x 2 (spills) 72; one CTA per two tokens, many more than fit: 84; without the streaming stores 72 at best.
+constexpr int kLookCtas = 6, kLookTokens = 2;
 template <typename T, int VEC, int U>
-__global__ void __launch_bounds__(kEmbThreads) emb_lookup_kernel(const T* __restrict__ table, int64_t rows, int64_t cols, int64_t ld, Ids ids, int64_t n,
+__global__ void __launch_bounds__(kEmbThreads, kLookCtas) emb_lookup_kernel(const T* __restrict__ table, int64_t rows, int64_t cols, int64_t ld, Ids ids, int64_t n,
                                                                  float scale, T* __restrict__ out, int64_t ld_out, int32_t* status) {
-  const int64_t col = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC;
-  const int64_t t0 = (int64_t)blockIdx.x * U * blockDim.y + threadIdx.y;
-  int64_t id[U];
+  const int64_t col = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC, step = (int64_t)gridDim.x * U * blockDim.y;
+  if (col >= cols) return;
+  int64_t id[U], t0 = (int64_t)blockIdx.x * U * blockDim.y + threadIdx.y;
 #pragma unroll
   for (int u = 0; u < U; ++u) { const int64_t t = t0 + (int64_t)u * blockDim.y; id[u] = t < n ? load_id(ids, t) : -1; }
-  if (col >= cols) return;
-  Pack<T, VEC> x[U];
+  for (; t0 < n; t0 += step) {
+    Pack<T, VEC> x[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (id[u] >= 0 && id[u] < rows) x[u] = load_pack<T, VEC>(table + id[u] * ld + col);
-    else {
+    for (int u = 0; u < U; ++u) {
+      if (id[u] >= 0 && id[u] < rows) x[u] = load_pack<T, VEC>(table + id[u] * ld + col);
+      else {
+        if (col == 0 && t0 + (int64_t)u * blockDim.y < n) raise_word(status);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) x[u].v[j] = from_float<T>(0.0f);
+        for (int j = 0; j < VEC; ++j) x[u].v[j] = from_float<T>(0.0f);
+      }
     }
-  }
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t t = t0 + (int64_t)u * blockDim.y;
-    if (t >= n) break;
-    if ((id[u] < 0 || id[u] >= rows) && col == 0) raise_word(status);
+    for (int u = 0; u < U; ++u) { const int64_t t = t0 + step + (int64_t)u * blockDim.y; id[u] = t < n ? load_id(ids, t) : -1; }      // the next ones, meanwhile
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) x[u].v[j] = from_float<T>(to_float(x[u].v[j]) * scale);
-    store_pack<T, VEC>(out + t * ld_out + col, x[u]);
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + (int64_t)u * blockDim.y;
+      if (t < n) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) x[u].v[j] = from_float<T>(to_float(x[u].v[j]) * scale);
+        if constexpr (VEC * sizeof(T) == 16) __stcs(reinterpret_cast<uint4*>(out + t * ld_out + col), *reinterpret_cast<uint4*>(&x[u]));
+        else store_pack<T, VEC>(out + t * ld_out + col, x[u]);
+      }
+    }
   }
 }
 
 // ---- sort -----------------------------------------------------------------------------------------
 struct SortArgs {
   Ids ids; int64_t n, rows, padding;
-  uint32_t *keys[2], *toks[2];          // the sorted pairs end in [passes & 1]
-  uint8_t* touched;                     // [rows] rows that have tokens
-  uint32_t* runs;                       // [0] number of runs that go over a chunk's end, then the chunks that they start in
+  uint64_t* items[2];                   // id << 32 | token; the sorted ones end in [passes & 1]
+  uint32_t* runs;                       // [0] number of long runs, then the chunks that they start in
   int32_t* status;
   int passes, bits;
   int64_t segment;                      // tokens of a CTA
+  uint32_t ctas;                        // CTAs that sort: the first cluster.  The others write rows without tokens:
+  float* out; int64_t cols, ld_out; int vec_out;
 };
 
 __device__ __forceinline__ void cluster_sync() {
@@ -95,61 +106,108 @@ __device__ __forceinline__ uint32_t remote_u32(const uint32_t* local, uint32_t r
   return v;
 }
 
-// an id as a sort key: ids that have no row, and the padding id, come last
-__device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int64_t t) {
+__device__ __forceinline__ void put_remote(uint64_t* local, uint32_t rank, uint64_t x) {
+  uint32_t a = (uint32_t)__cvta_generic_to_shared(local), r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(r), "l"(x) : "memory");
+}
+
+// a token as a sort item: ids that have no row, and the padding id, come last
+__device__ __forceinline__ uint64_t sort_item(const SortArgs& a, int64_t t) {
   const int64_t id = load_id(a.ids, t);
   const bool ok = id >= 0 && id < a.rows;
   if (!ok) raise_word(a.status);
-  return ok && id != a.padding ? (uint32_t)id : (uint32_t)a.rows;
+  return (uint64_t)(ok && id != a.padding ? (uint32_t)id : (uint32_t)a.rows) << 32 | (uint32_t)t;
 }
 
-// ONE: a CTA's segment fits one tile, whose ranks stay in registers
+// a run is long if it goes on behind the chunk that follows the one it starts in
+__device__ __forceinline__ uint32_t item_id(const uint64_t* items, int64_t i) { return (uint32_t)(items[i] >> 32); }
+
+// rows without tokens, by the CTAs behind those that sort: a range of rows each
+__device__ __forceinline__ void zero_rows(const SortArgs& a, uint8_t* s_seen) {
+  constexpr int64_t kFlags = 65536;
+  const int64_t per = (a.rows + (gridDim.x - a.ctas) - 1) / (gridDim.x - a.ctas);
+  const int64_t begin = (int64_t)(blockIdx.x - a.ctas) * per, end = min(begin + per, a.rows);
+  for (int64_t r0 = begin; r0 < end; r0 += kFlags) {
+    const int64_t count = min(kFlags, end - r0);
+    for (int64_t i = threadIdx.x; i < count; i += kSortThreads) s_seen[i] = 0;
+    __syncthreads();
+#pragma unroll 8
+    for (int64_t t = threadIdx.x; t < a.n; t += kSortThreads) {
+      const int64_t id = load_id(a.ids, t);
+      if (id >= r0 && id < r0 + count && id != a.padding) s_seen[id - r0] = 1;
+    }
+    __syncthreads();
+    for (int64_t r = threadIdx.x >> 5; r < count; r += kSortWarps) {
+      if (s_seen[r]) continue;
+      float* p = a.out + (r0 + r) * a.ld_out;
+      int64_t c = threadIdx.x & 31;
+      if (a.vec_out) {
+        for (; c < a.cols / 4; c += 32) reinterpret_cast<float4*>(p)[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        c = a.cols / 4 * 4 + (threadIdx.x & 31);
+      }
+      for (; c < a.cols; c += 32) p[c] = 0.0f;
+    }
+    __syncthreads();
+  }
+}
+
+// ONE: a CTA's segment fits one tile: its items stay in registers between ranking and writing, and between passes in the shared memory of the CTAs that
+// rank them next.  Longer lists go through L2, a tile at a time.  (Lanes with equal digits are found by eight votes: the match instruction took
+// 1.3 k cycles per item and warp of a CTA of 32.)
 template <bool ONE>
-__global__ void __launch_bounds__(kSortThreads, 1) emb_sort_kernel(SortArgs a) {
+__global__ void __launch_bounds__(kSortThreads, 1) emb_sort_kernel(const __grid_constant__ SortArgs a) {
+  extern __shared__ uint64_t s_items[];                          // [kSortTile] the tile in order; ONE: [kSortTile] what the next pass ranks
+  uint64_t* s_next = s_items + kSortTile;
   __shared__ uint16_t s_warp[kSortWarps][256];                   // a digit's items per warp, then before the warp
-  __shared__ uint32_t s_hist[256], s_base[256], s_tile[256], s_scan[8];
+  __shared__ uint32_t s_hist[256], s_base[256], s_tile[256], s_first[256], s_scan[2][8];   // s_first: of a digit in the ordered tile
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int64_t begin = min((int64_t)blockIdx.x * a.segment, a.n), end = min(begin + a.segment, a.n);
-  for (int64_t i = (int64_t)blockIdx.x * kSortThreads + tid; i < a.rows; i += (int64_t)gridDim.x * kSortThreads) a.touched[i] = 0;
+  if (blockIdx.x >= a.ctas) return zero_rows(a, reinterpret_cast<uint8_t*>(s_items));
   if (blockIdx.x == 0 && tid == 0) a.runs[0] = 0;
-  uint32_t key[kSortItems], tok[kSortItems], rank[kSortItems];
+  uint64_t item[kSortItems];
+  uint32_t rank[kSortItems];
   for (int pass = 0; pass < a.passes; ++pass) {
-    const int shift = pass * a.bits;
+    const int shift = 32 + pass * a.bits;
     const uint32_t mask = (1u << a.bits) - 1u;
-    const uint32_t* src_k = a.keys[pass & 1];
-    const uint32_t* src_t = a.toks[pass & 1];
-    uint32_t* dst_k = a.keys[(pass + 1) & 1];
-    uint32_t* dst_t = a.toks[(pass + 1) & 1];
-    // items of a tile: warp by warp, each 32 x `items` of them in order
+    const uint64_t* src = a.items[pass & 1];
+    uint64_t* dst = a.items[(pass + 1) & 1];
+    const bool last = pass + 1 == a.passes;
+    // items of a tile: warp by warp, each 32 x `per` of them in order
     auto load_tile = [&](int64_t t0) {
-      const int items = (int)((min((int64_t)kSortTile, end - t0) + kSortThreads - 1) / kSortThreads);
+      const int per = (int)((min((int64_t)kSortTile, end - t0) + kSortThreads - 1) / kSortThreads);
 #pragma unroll
       for (int j = 0; j < kSortItems; ++j) {
-        if (j >= items) break;
-        const int64_t t = t0 + (int64_t)warp * 32 * items + j * 32 + lane;
-        tok[j] = 0xffffffffu; key[j] = 0u;
-        if (t < end) { key[j] = pass == 0 ? sort_key(a, t) : src_k[t]; tok[j] = pass == 0 ? (uint32_t)t : src_t[t]; }
+        if (j < per) {
+          const int64_t t = t0 + (int64_t)warp * 32 * per + j * 32 + lane;
+          item[j] = t < end ? (pass == 0 ? sort_item(a, t) : ONE ? s_next[t - begin] : src[t]) : 0u;
+        }
       }
-      return items;
+      return per;
     };
     // rank of every item among those of its digit in its warp; s_warp = items of a digit in the warps before, s_tile = in the tile
-    auto rank_tile = [&](int64_t t0, int items) {
-      uint4* row = reinterpret_cast<uint4*>(s_warp[warp]);
-      row[lane] = make_uint4(0u, 0u, 0u, 0u);
+    auto rank_tile = [&](int64_t t0, int per) {
+      reinterpret_cast<uint4*>(s_warp[warp])[lane] = make_uint4(0u, 0u, 0u, 0u);
       __syncwarp();
 #pragma unroll
       for (int j = 0; j < kSortItems; ++j) {
-        if (j >= items) break;
-        const bool valid = t0 + (int64_t)warp * 32 * items + j * 32 + lane < end;
-        const uint32_t digit = valid ? (key[j] >> shift) & mask : 0xffffffffu;
-        const uint32_t peers = __match_any_sync(0xffffffffu, digit);
-        const uint32_t below = __popc(peers & ((1u << lane) - 1u));
-        uint32_t before = 0u;
-        if (valid) before = s_warp[warp][digit];
-        __syncwarp();
-        if (valid && below == 0u) s_warp[warp][digit] = (uint16_t)(before + __popc(peers));
-        __syncwarp();
-        rank[j] = before + below;
+        if (j < per) {
+          const bool valid = t0 + (int64_t)warp * 32 * per + j * 32 + lane < end;
+          const uint32_t digit = (uint32_t)(item[j] >> shift) & mask;
+          uint32_t peers = __ballot_sync(0xffffffffu, valid);              // lanes with the same digit
+#pragma unroll
+          for (int b = 0; b < 8; ++b) {
+            const uint32_t set = __ballot_sync(0xffffffffu, digit >> b & 1u);
+            peers &= digit >> b & 1u ? set : ~set;
+          }
+          const uint32_t below = __popc(peers & ((1u << lane) - 1u));
+          uint32_t before = 0u;
+          if (valid) before = s_warp[warp][digit];
+          __syncwarp();
+          if (valid && below == 0u) s_warp[warp][digit] = (uint16_t)(before + __popc(peers));
+          __syncwarp();
+          rank[j] = before + below;
+        }
       }
       __syncthreads();
       if (tid < 256) {
@@ -158,53 +216,77 @@ __global__ void __launch_bounds__(kSortThreads, 1) emb_sort_kernel(SortArgs a) {
         for (int w = 0; w < kSortWarps; ++w) { const uint32_t c = s_warp[w][tid]; s_warp[w][tid] = (uint16_t)run; run += c; }
         s_tile[tid] = run;
       }
-      __syncthreads();
     };
-    auto scatter_tile = [&](int64_t t0, int items) {
+    // exclusive sums over the 256 digits of v, by the first 256 threads; all threads meet
+    auto scan = [&](uint32_t v, uint32_t* s) {
+      uint32_t x = v;
+      if (tid < 256) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+        if (lane == 31) s[warp] = x;
+      }
+      __syncthreads();
+      if (tid < 256) for (int w = 0; w < warp; ++w) x += s[w];
+      return x - v;
+    };
+    // the tile in order into shared memory, from there in runs to its places (s_base: the digit's first)
+    auto write_tile = [&](int64_t t0, int per) {
+      const uint32_t first = scan(tid < 256 ? s_tile[tid] : 0u, s_scan[0]);
+      if (tid < 256) s_first[tid] = first;
+      __syncthreads();
 #pragma unroll
       for (int j = 0; j < kSortItems; ++j) {
-        if (j >= items) break;
-        if (t0 + (int64_t)warp * 32 * items + j * 32 + lane < end) {
-          const uint32_t digit = (key[j] >> shift) & mask;
-          const uint32_t at = s_base[digit] + s_warp[warp][digit] + rank[j];
-          dst_k[at] = key[j]; dst_t[at] = tok[j];
-          if (pass + 1 == a.passes && key[j] < (uint32_t)a.rows) a.touched[key[j]] = 1;
+        if (j < per && t0 + (int64_t)warp * 32 * per + j * 32 + lane < end) {
+          const uint32_t digit = (uint32_t)(item[j] >> shift) & mask;
+          s_items[s_first[digit] + s_warp[warp][digit] + rank[j]] = item[j];
+        }
+      }
+      __syncthreads();
+      const int count = (int)min((int64_t)kSortTile, end - t0);
+#pragma unroll
+      for (int j = 0; j < kSortItems; ++j) {
+        const int i = j * kSortThreads + tid;
+        if (i < count) {
+          const uint64_t x = s_items[i];
+          const uint32_t digit = (uint32_t)(x >> shift) & mask;
+          const uint32_t at = s_base[digit] + (i - s_first[digit]);
+          if (ONE && !last) {
+            const uint32_t cta = at / (uint32_t)a.segment;
+            put_remote(s_next + (at - cta * (uint32_t)a.segment), cta, x);
+          } else dst[at] = x;
         }
       }
     };
-    int items = 0;
+    int per = 0;
     if (tid < 256) s_hist[tid] = 0u;
     if constexpr (ONE) {
-      if (begin < end) { items = load_tile(begin); rank_tile(begin, items); if (tid < 256) s_hist[tid] = s_tile[tid]; }
+      if (begin < end) { per = load_tile(begin); rank_tile(begin, per); if (tid < 256) s_hist[tid] = s_tile[tid]; }
     } else {
       for (int64_t t0 = begin; t0 < end; t0 += kSortTile) {
-        items = load_tile(t0); rank_tile(t0, items);
+        per = load_tile(t0); rank_tile(t0, per);
         if (tid < 256) s_hist[tid] += s_tile[tid];
+        __syncthreads();
       }
     }
     cluster_sync();
     // first place of this CTA's items of a digit: all items of smaller digits, and those of this one in the CTAs before
-    uint32_t below = 0, total = 0, scan = 0;
+    uint32_t below = 0, total = 0;
     if (tid < 256) {
-      for (uint32_t b = 0; b < gridDim.x; ++b) { const uint32_t c = remote_u32(&s_hist[tid], b); if (b < blockIdx.x) below += c; total += c; }
-      scan = total;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, scan, o); if (lane >= o) scan += v; }
-      if (lane == 31) s_scan[warp] = scan;
+      for (uint32_t b = 0; b < kSortClusterMax; ++b) {
+        if (b < a.ctas) { const uint32_t c = remote_u32(&s_hist[tid], b); if (b < blockIdx.x) below += c; total += c; }
+      }
     }
-    __syncthreads();
-    if (tid < 256) {
-      uint32_t before = 0;
-      for (int w = 0; w < warp; ++w) before += s_scan[w];
-      s_base[tid] = before + scan - total + below;
-    }
-    __syncthreads();
+    const uint32_t smaller = scan(total, s_scan[1]);
+    if (tid < 256) s_base[tid] = smaller + below;
     if constexpr (ONE) {
-      if (begin < end) scatter_tile(begin, items);
+      if (begin < end) write_tile(begin, per);
     } else {
+      __syncthreads();
       for (int64_t t0 = begin; t0 < end; t0 += kSortTile) {
-        items = load_tile(t0); rank_tile(t0, items);
-        scatter_tile(t0, items);
+        per = load_tile(t0); rank_tile(t0, per);
+        __syncthreads();
+        write_tile(t0, per);
         __syncthreads();
         if (tid < 256) s_base[tid] += s_tile[tid];
         __syncthreads();
@@ -212,25 +294,23 @@ __global__ void __launch_bounds__(kSortThreads, 1) emb_sort_kernel(SortArgs a) {
     }
     cluster_sync();
   }
-  // runs that go over the end of the chunk that they start in
-  const uint32_t* keys = a.keys[a.passes & 1];
+  // the long runs, by the chunk that they start in
+  const uint64_t* items = a.items[a.passes & 1];
   const int64_t chunks = (a.n + kEmbChunk - 1) / kEmbChunk;
-  for (int64_t c = (int64_t)blockIdx.x * kSortThreads + tid; c + 1 < chunks; c += (int64_t)gridDim.x * kSortThreads) {
-    const uint32_t k = keys[c * kEmbChunk + kEmbChunk - 1];
-    if (k < (uint32_t)a.rows && keys[(c + 1) * kEmbChunk] == k && (c == 0 || keys[c * kEmbChunk - 1] != k)) a.runs[1 + atomicAdd(&a.runs[0], 1u)] = (uint32_t)c;
+  for (int64_t c = (int64_t)blockIdx.x * kSortThreads + tid; c + 2 < chunks; c += (int64_t)a.ctas * kSortThreads) {
+    const uint32_t k = item_id(items, (c + 1) * kEmbChunk - 1);
+    if (k < (uint32_t)a.rows && item_id(items, (c + 2) * kEmbChunk) == k && (c == 0 || item_id(items, c * kEmbChunk - 1) != k)) a.runs[1 + atomicAdd(&a.runs[0], 1u)] = (uint32_t)c;
   }
 }
 
 // ---- sums -----------------------------------------------------------------------------------------
 struct SumArgs {
-  const uint32_t *keys, *toks; const uint8_t* touched; const uint32_t* runs;
+  const uint64_t* items; const uint32_t* runs;
   int64_t n, chunks, rows, cols;
   const void* dout; int64_t ld;
   float scale; int accumulate;
   float* out; int64_t ld_out;
-  float* parts; int64_t ld_part;       // [chunks][2][ld_part]: the part of a run that came over the chunk's start, of one that goes over its end
-  int64_t sum_ctas;                    // CTAs (along x) that sum; the others write rows without tokens
-  int zero_rows;                       // rows of one of those
+  float* parts; int64_t ld_part;       // [chunks][2][ld_part]: the part of a long run that came over the chunk's start, of one that goes over its end
   int vec_out;                         // out may be moved 16 bytes at a time
 };
 
@@ -250,103 +330,115 @@ __device__ __forceinline__ void put_row(const SumArgs& a, float* p, const float 
   }
 }
 
+// A thread's packs of the gradient's rows on their way: kAhead of them, each thread's own, so that it waits for nobody else's.
+// 16- and 4-byte packs are copied to shared memory asynchronously, which takes no registers; 2-byte ones are loaded.
+template <typename T, int VEC, int AHEAD>
+struct RowQueue {
+  static constexpr int kBytes = VEC * (int)sizeof(T);
+  static constexpr bool kAsync = kBytes == 16 || kBytes == 4;
+  Pack<T, VEC>* slot; int stride;      // of this thread; packs between two of its slots
+  __device__ __forceinline__ void put(int i, const T* p) {
+    Pack<T, VEC>* s = slot + (i % AHEAD) * stride;
+    if constexpr (kAsync) copy_async<kBytes>(s, p);
+    else *s = load_pack<T, VEC>(p);
+  }
+  __device__ __forceinline__ void close() { if constexpr (kAsync) asm volatile("cp.async.commit_group;" ::: "memory"); }
+  __device__ __forceinline__ Pack<T, VEC> get(int i) {
+    if constexpr (kAsync) asm volatile("cp.async.wait_group %0;" :: "n"(AHEAD - 1) : "memory");
+    return slot[(i % AHEAD) * stride];
+  }
+};
+
+constexpr int kEmbAhead = 12, kWindow = 3 * kEmbChunk + 2;
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kEmbThreads) emb_sum_kernel(SumArgs a) {
-  constexpr int kAhead = 8;
-  extern __shared__ uint32_t s_chunk[];                           // [cy][2][kEmbChunk] keys, tokens
+__global__ void __launch_bounds__(kEmbThreads, 4) emb_sum_kernel(const __grid_constant__ SumArgs a) {
+  extern __shared__ uint4 s_raw[];     // [kEmbAhead][threads] packs, then [cy][kWindow] items
   wait_for_previous();
   const int tid = threadIdx.y * blockDim.x + threadIdx.x, threads = blockDim.x * blockDim.y;
   const int64_t col = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC;
-  if ((int64_t)blockIdx.x >= a.sum_ctas) {
-    const int64_t r0 = ((int64_t)blockIdx.x - a.sum_ctas) * a.zero_rows;
-    if (col >= a.cols) return;
-    for (int64_t r = r0 + threadIdx.y; r < min(r0 + a.zero_rows, a.rows); r += blockDim.y) {
-      if (a.n > 0 && a.touched[r]) continue;
-      float* p = a.out + r * a.ld_out + col;
-      if (VEC % 4 == 0 && a.vec_out) {
-#pragma unroll
-        for (int j = 0; j < VEC; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      } else {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) p[j] = 0.0f;
-      }
-    }
-    return;
-  }
-  for (int i = tid; i < (int)blockDim.y * kEmbChunk; i += threads) {
-    const int64_t at = (int64_t)blockIdx.x * blockDim.y * kEmbChunk + i;
-    const int y = i / kEmbChunk, k = i % kEmbChunk;
-    s_chunk[(y * 2) * kEmbChunk + k] = at < a.n ? a.keys[at] : 0xffffffffu;
-    s_chunk[(y * 2 + 1) * kEmbChunk + k] = at < a.n ? a.toks[at] : 0u;
+  uint64_t* s_items = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_raw) + (size_t)kEmbAhead * threads * VEC * sizeof(T));
+  for (int i = tid; i < (int)blockDim.y * kWindow; i += threads) {
+    const int64_t at = ((int64_t)blockIdx.x * blockDim.y + i / kWindow - 1) * kEmbChunk + i % kWindow - 1;
+    s_items[i] = at >= 0 && at < a.n ? a.items[at] : ~0ull;
   }
   __syncthreads();
   const int64_t chunk = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   if (chunk >= a.chunks || col >= a.cols) return;
   const int64_t first = chunk * kEmbChunk;
-  const int count = (int)min((int64_t)kEmbChunk, a.n - first);
-  const uint32_t* keys = s_chunk + threadIdx.y * 2 * kEmbChunk;
-  const uint32_t* toks = keys + kEmbChunk;
-  const uint32_t before = first > 0 ? a.keys[first - 1] : 0xffffffffu, behind = first + count < a.n ? a.keys[first + count] : 0xffffffffu;
+  const uint64_t* items = s_items + threadIdx.y * kWindow + kEmbChunk + 1;      // of this chunk; a chunk and one token before, two chunks behind
+  auto id_at = [&](int i) { return (uint32_t)(items[i] >> 32); };
+  int begin = 0, end = (int)min((int64_t)kEmbChunk, a.n - first);
+  // the run at the chunk's start: skipped if the chunk before sums it, else a part; the one at its end: followed into the next chunk, or a part
+  const uint32_t head = id_at(0), tail = id_at(end - 1);
+  const bool head_part = id_at(-1) == head;
+  bool tail_part = false;
+  if (head_part && id_at(kEmbChunk) != head && id_at(-kEmbChunk - 1) != head) {
+    while (begin < end && id_at(begin) == head) ++begin;
+  }
+  if (end == kEmbChunk && tail < (uint32_t)a.rows && id_at(kEmbChunk) == tail && !(head_part && head == tail)) {
+    tail_part = id_at(2 * kEmbChunk) == tail;
+    if (!tail_part) while (end < 2 * kEmbChunk && id_at(end) == tail) ++end;
+  }
+  while (begin < end && id_at(end - 1) >= (uint32_t)a.rows) --end;             // tokens that are left out come last
+  if (begin >= end) return;
   const T* dout = static_cast<const T*>(a.dout) + col;
+  RowQueue<T, VEC, kEmbAhead> queue{reinterpret_cast<Pack<T, VEC>*>(s_raw) + tid, threads};
+#pragma unroll
+  for (int i = 0; i < kEmbAhead - 1; ++i) {
+    if (begin + i < end) queue.put(i, dout + (int64_t)(uint32_t)items[begin + i] * a.ld);
+    queue.close();
+  }
   float acc[VEC];
 #pragma unroll
   for (int j = 0; j < VEC; ++j) acc[j] = 0.0f;
-  uint32_t run = keys[0];
-  bool came_over = run == before;
-  auto flush = [&](bool goes_over) {
-    if (run < (uint32_t)a.rows) {
-      if (came_over || goes_over) {
-        float* p = a.parts + (chunk * 2 + (came_over ? 0 : 1)) * a.ld_part + col;
+  uint32_t run = id_at(begin);
+  bool part = head_part && begin == 0;
+  auto flush = [&](int slot) {
+    if (slot >= 0) {
+      float* p = a.parts + (chunk * 2 + slot) * a.ld_part + col;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) p[j] = acc[j];
-      } else put_row<VEC>(a, a.out + (int64_t)run * a.ld_out + col, acc);
-    }
+      for (int j = 0; j < VEC; ++j) p[j] = acc[j];
+    } else put_row<VEC>(a, a.out + (int64_t)run * a.ld_out + col, acc);
   };
-  for (int i0 = 0; i0 < count; i0 += kAhead) {
-    Pack<T, VEC> x[kAhead];
+  for (int i = begin; i < end; ++i) {
+    const int ahead = i + kEmbAhead - 1;
+    if (ahead < end) queue.put(ahead - begin, dout + (int64_t)(uint32_t)items[ahead] * a.ld);
+    queue.close();
+    const Pack<T, VEC> x = queue.get(i - begin);
+    const uint32_t id = id_at(i);
+    if (id != run) {
+      flush(part ? 0 : -1);
+      run = id; part = false;
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u)
-      if (i0 + u < count && keys[i0 + u] < (uint32_t)a.rows) x[u] = load_pack<T, VEC>(dout + (int64_t)toks[i0 + u] * a.ld);
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (i0 + u >= count) break;
-      const uint32_t k = keys[i0 + u];
-      if (k != run) {
-        flush(false);
-        run = k; came_over = false;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) acc[j] = 0.0f;
-      }
-      if (k < (uint32_t)a.rows) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) acc[j] += to_float(x[u].v[j]);
-      }
+      for (int j = 0; j < VEC; ++j) acc[j] = 0.0f;
     }
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) acc[j] += to_float(x.v[j]);
   }
-  flush(run == behind);
+  flush(part ? 0 : tail_part ? 1 : -1);
 }
 
-// A CTA adds the parts of one run for 128 columns: eight slices of the run's chunks, then the slices.
+// A CTA adds the parts of one long run for 128 columns: eight slices of the run's chunks, then the slices.
 constexpr int kJoinSlices = 8;
-__global__ void __launch_bounds__(32 * kJoinSlices) emb_join_kernel(SumArgs a) {
+__global__ void __launch_bounds__(32 * kJoinSlices) emb_join_kernel(const __grid_constant__ SumArgs a) {
   __shared__ float4 s_part[kJoinSlices][32];
-  __shared__ int64_t s_last;
   wait_for_previous();
   const int64_t slabs = (a.cols + 127) / 128, units = (int64_t)a.runs[0] * slabs;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int64_t c0 = a.runs[1 + unit / slabs], col = (unit % slabs) * 128 + threadIdx.x * 4;
-    const uint32_t k = a.keys[c0 * kEmbChunk + kEmbChunk - 1];
-    if (threadIdx.x == 0 && threadIdx.y == 0) {                   // last chunk that starts with this id: the keys ascend
-      int64_t lo = c0 + 1, hi = a.chunks - 1;
-      while (lo < hi) { const int64_t mid = (lo + hi + 1) >> 1; if (a.keys[mid * kEmbChunk] == k) lo = mid; else hi = mid - 1; }
-      s_last = lo;
+    const uint32_t k = item_id(a.items, (c0 + 1) * kEmbChunk - 1);
+    int64_t count = 1;                                            // the chunks that have a part: those that start with this id (the ids ascend)
+    for (;;) {
+      const int64_t c = c0 + count + threadIdx.y * 32 + threadIdx.x;
+      const int more = __syncthreads_count(c < a.chunks && item_id(a.items, c * kEmbChunk) == k);
+      count += more;
+      if (more < 32 * kJoinSlices) break;
     }
-    __syncthreads();
-    const int64_t count = s_last - c0 + 1, per = (count + kJoinSlices - 1) / kJoinSlices;
+    const int64_t per = (count + kJoinSlices - 1) / kJoinSlices;
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (col < a.cols) {
       const int64_t i1 = min(count, (threadIdx.y + 1) * per);
-#pragma unroll 4
+#pragma unroll 8
       for (int64_t i = threadIdx.y * per; i < i1; ++i) {
         const float4 x = *reinterpret_cast<const float4*>(a.parts + ((c0 + i) * 2 + (i == 0 ? 1 : 0)) * a.ld_part + col);
         acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
@@ -360,7 +452,10 @@ __global__ void __launch_bounds__(32 * kJoinSlices) emb_join_kernel(SumArgs a) {
       for (int s = 0; s < kJoinSlices; ++s) { const float4 v = s_part[s][threadIdx.x]; x[0] += v.x; x[1] += v.y; x[2] += v.z; x[3] += v.w; }
       float* p = a.out + (int64_t)k * a.ld_out + col;
       if (col + 3 < a.cols) put_row<4>(a, p, x);
-      else for (int64_t j = 0; col + j < a.cols; ++j) { const float y[1] = {x[j]}; put_row<1>(a, p + j, y); }
+      else {
+#pragma unroll
+        for (int j = 0; j < 3; ++j) if (col + j < a.cols) { const float y[1] = {x[j]}; put_row<1>(a, p + j, y); }
+      }
     }
     __syncthreads();
   }
@@ -378,12 +473,12 @@ template <typename T, int VEC>
 cudaError_t lookup_typed(const EmbLookup& a, cudaStream_t st) {
   const EmbShape s = emb_shape(a.cols, VEC);
   const dim3 block(s.cx, s.cy);
-  // four tokens per thread from where a quarter as many threads still fill the GPU
-  const bool many = a.n * s.slabs * s.cx / 4 >= 148 * 2048;
-  const int u = many ? 4 : 1;
-  const dim3 grid((unsigned)((a.n + (int64_t)s.cy * u - 1) / ((int64_t)s.cy * u)), s.slabs);
+  // several tokens at a time from where so many fewer threads still fill the GPU
+  const bool many = a.n * s.slabs * s.cx / kLookTokens >= 148 * 2048;
+  const int64_t per = (int64_t)s.cy * (many ? kLookTokens : 1);
+  const dim3 grid((unsigned)std::min<int64_t>((a.n + per - 1) / per, many ? std::max(1, 148 * kLookCtas / s.slabs) : (int64_t)1 << 30), s.slabs);
   const Ids ids{a.ids, a.id_bytes == 8};
-  if (many) emb_lookup_kernel<T, VEC, 4><<<grid, block, 0, st>>>((const T*)a.table, a.rows, a.cols, a.ld, ids, a.n, a.scale, (T*)a.out, a.ld_out, a.status);
+  if (many) emb_lookup_kernel<T, VEC, kLookTokens><<<grid, block, 0, st>>>((const T*)a.table, a.rows, a.cols, a.ld, ids, a.n, a.scale, (T*)a.out, a.ld_out, a.status);
   else emb_lookup_kernel<T, VEC, 1><<<grid, block, 0, st>>>((const T*)a.table, a.rows, a.cols, a.ld, ids, a.n, a.scale, (T*)a.out, a.ld_out, a.status);
   return cudaGetLastError();
 }
@@ -395,30 +490,39 @@ cudaError_t lookup_type(const EmbLookup& a, cudaStream_t st) {
   return lookup_typed<T, 1>(a, st);
 }
 
-struct EmbLayout { uint64_t keys[2], toks[2], touched, runs, parts, bytes; int64_t chunks, ld_part; };
-EmbLayout emb_layout(int64_t n, int64_t rows, int64_t cols) {
+struct EmbLayout { uint64_t items[2], runs, parts, bytes; int64_t chunks, ld_part; };
+EmbLayout emb_layout(int64_t n, int64_t cols) {
   EmbLayout l{};
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) { const uint64_t p = at; at = align_up(at + bytes, 256); return p; };
   l.chunks = (n + kEmbChunk - 1) / kEmbChunk;
   l.ld_part = (cols + 3) / 4 * 4;
-  for (int i = 0; i < 2; ++i) { l.keys[i] = take((uint64_t)n * 4); l.toks[i] = take((uint64_t)n * 4); }
-  l.touched = take((uint64_t)rows);
+  for (int i = 0; i < 2; ++i) l.items[i] = take((uint64_t)n * 8);
   l.runs = take((uint64_t)(l.chunks + 1) * 4);
   l.parts = take((uint64_t)l.chunks * 2 * l.ld_part * 4);
   l.bytes = at;
   return l;
 }
 
+// clusters of 1, 2, .. 16 CTAs that the GPU holds side by side, by device
+struct SortRoom { int clusters[5]; } sort_room[64];
+
+struct SortLaunch {
+  cudaLaunchAttribute attr[1];
+  cudaLaunchConfig_t cfg = {};
+  SortLaunch(int cluster, int grid, size_t smem, cudaStream_t st) {
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(kSortThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 1;
+  }
+  SortLaunch(const SortLaunch&) = delete;
+};
+
 template <typename T, int VEC>
 cudaError_t sum_typed(SumArgs& a, cudaStream_t st) {
   const EmbShape s = emb_shape(a.cols, VEC);
-  a.sum_ctas = (a.chunks + s.cy - 1) / s.cy;
-  // rows of a CTA that writes zeros: about 64 KB of them
-  a.zero_rows = (int)std::max<int64_t>(s.cy, std::min<int64_t>(1024, 65536 / (4 * std::min<int64_t>(a.cols, (int64_t)s.cx * VEC))));
-  const int64_t zero_ctas = a.accumulate ? 0 : (a.rows + a.zero_rows - 1) / a.zero_rows;
-  if (a.sum_ctas + zero_ctas == 0) return cudaSuccess;
-  return launch_after(emb_sum_kernel<T, VEC>, dim3((unsigned)(a.sum_ctas + zero_ctas), s.slabs), dim3(s.cx, s.cy), (size_t)s.cy * 2 * kEmbChunk * 4, st, a);
+  const size_t smem = (size_t)kEmbAhead * s.cx * s.cy * VEC * sizeof(T) + (size_t)s.cy * kWindow * 8;
+  return launch_after(emb_sum_kernel<T, VEC>, dim3((unsigned)((a.chunks + s.cy - 1) / s.cy), s.slabs), dim3(s.cx, s.cy), smem, st, a);
 }
 template <typename T>
 cudaError_t sum_type(SumArgs& a, cudaStream_t st) {
@@ -430,6 +534,27 @@ cudaError_t sum_type(SumArgs& a, cudaStream_t st) {
 
 }  // namespace
 
+int embedding_configure(int device) {
+  cudaError_t e = cudaFuncSetAttribute(emb_sort_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortTile * 16);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(emb_sort_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortTile * 8);
+  // up to 48 KB of packs in flight and 25 KB of items
+  auto sum = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 80 * 1024); };
+  sum(emb_sum_kernel<float, 4>); sum(emb_sum_kernel<float, 1>);
+  sum(emb_sum_kernel<__nv_bfloat16, 8>); sum(emb_sum_kernel<__nv_bfloat16, 2>); sum(emb_sum_kernel<__nv_bfloat16, 1>);
+  sum(emb_sum_kernel<__half, 8>); sum(emb_sum_kernel<__half, 2>); sum(emb_sum_kernel<__half, 1>);
+  if (e != cudaSuccess) return (int)e;
+  const bool wide = cudaFuncSetAttribute(emb_sort_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                    cudaFuncSetAttribute(emb_sort_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+  for (int lg = 0; lg <= 4; ++lg) {
+    int clusters = 0;
+    const SortLaunch l(1 << lg, 1 << lg, kSortTile * 16, nullptr);
+    if ((lg < 4 || wide) && cudaOccupancyMaxActiveClusters(&clusters, emb_sort_kernel<true>, &l.cfg) != cudaSuccess) clusters = 0;
+    sort_room[device & 63].clusters[lg] = clusters;
+  }
+  cudaGetLastError();
+  return 0;
+}
+
 int launch_embedding(const EmbLookup& a, cudaStream_t st) {
   if (a.n == 0) return (int)cudaSuccess;
   if (a.type == ATOMO_TYPE_F32) return (int)lookup_type<float>(a, st);
@@ -437,39 +562,46 @@ int launch_embedding(const EmbLookup& a, cudaStream_t st) {
   return (int)lookup_type<__half>(a, st);
 }
 
-uint64_t embedding_workspace(int64_t n, int64_t rows, int64_t cols) { return emb_layout(n, rows, cols).bytes; }
+uint64_t embedding_workspace(int64_t n, int64_t cols) { return emb_layout(n, cols).bytes; }
 
 int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
-  const EmbLayout l = emb_layout(b.n, b.rows, b.cols);
+  if (b.n == 0 && b.accumulate) return (int)cudaSuccess;
+  const EmbLayout l = emb_layout(b.n, b.cols);
+  const int vec_out = reinterpret_cast<uintptr_t>(b.out) % 16 == 0 && b.ld_out % 4 == 0;
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return (int)e;
+  SortArgs s{};
+  s.ids = Ids{b.ids, b.id_bytes == 8}; s.n = b.n; s.rows = b.rows; s.padding = b.padding; s.status = b.status;
+  for (int i = 0; i < 2; ++i) s.items[i] = reinterpret_cast<uint64_t*>(b.ws + l.items[i]);
+  s.runs = reinterpret_cast<uint32_t*>(b.ws + l.runs);
+  s.out = b.out; s.cols = b.cols; s.ld_out = b.ld_out; s.vec_out = vec_out;
+  int bits = 1;
+  while ((b.rows >> bits) != 0) ++bits;                          // ids as sort keys are 0 .. rows
+  s.passes = (bits + 7) / 8; s.bits = (bits + s.passes - 1) / s.passes;
+  // a token per thread up to the cluster's size
+  const SortRoom& room = sort_room[device & 63];
+  int lg = 0;
+  while (lg < 4 && ((int64_t)kSortThreads << lg) < b.n && room.clusters[lg + 1] > 0) ++lg;
+  const int ctas = 1 << lg;
+  s.ctas = (uint32_t)ctas;
+  s.segment = (b.n + ctas - 1) / ctas;
+  // the clusters that run beside it, for the rows without tokens; fewer where a CTA would have less than 16 KB of them
+  const int64_t most = b.accumulate ? 0 : std::max<int64_t>(1, b.rows * b.cols / 4096);
+  const int64_t others = std::min<int64_t>(std::max(1, room.clusters[lg] - 1), (most + ctas - 1) / ctas) * ctas;
+  const size_t smem = s.segment <= kSortTile ? kSortTile * 16 : kSortTile * 8;
+  const SortLaunch launch(ctas, (int)(ctas + others), smem, st);
+  e = s.segment <= kSortTile ? cudaLaunchKernelEx(&launch.cfg, emb_sort_kernel<true>, s) : cudaLaunchKernelEx(&launch.cfg, emb_sort_kernel<false>, s);
+  if (e != cudaSuccess || b.n == 0) return (int)e;
   SumArgs a{};
+  a.items = s.items[s.passes & 1]; a.runs = s.runs;
   a.n = b.n; a.chunks = l.chunks; a.rows = b.rows; a.cols = b.cols;
-  a.dout = b.grad; a.ld = b.ld; a.scale = b.scale; a.accumulate = b.accumulate; a.out = b.out; a.ld_out = b.ld_out; a.ld_part = l.ld_part;
-  a.vec_out = reinterpret_cast<uintptr_t>(b.out) % 16 == 0 && b.ld_out % 4 == 0;
-  if (b.n > 0) {
-    SortArgs s{};
-    s.ids = Ids{b.ids, b.id_bytes == 8}; s.n = b.n; s.rows = b.rows; s.padding = b.padding; s.status = b.status;
-    for (int i = 0; i < 2; ++i) { s.keys[i] = reinterpret_cast<uint32_t*>(b.ws + l.keys[i]); s.toks[i] = reinterpret_cast<uint32_t*>(b.ws + l.toks[i]); }
-    s.touched = b.ws + l.touched;
-    s.runs = reinterpret_cast<uint32_t*>(b.ws + l.runs);
-    int bits = 1;
-    while ((b.rows >> bits) != 0) ++bits;                        // keys are 0 .. rows
-    s.passes = (bits + 7) / 8; s.bits = (bits + s.passes - 1) / s.passes;
-    const int ctas = b.n <= kSortThreads ? 1 : kSortCluster;
-    s.segment = (b.n + ctas - 1) / ctas;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(kSortThreads); cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 1;
-    const cudaError_t e = s.segment <= kSortTile ? cudaLaunchKernelEx(&cfg, emb_sort_kernel<true>, s) : cudaLaunchKernelEx(&cfg, emb_sort_kernel<false>, s);
-    if (e != cudaSuccess) return (int)e;
-    a.keys = s.keys[s.passes & 1]; a.toks = s.toks[s.passes & 1]; a.touched = s.touched; a.runs = s.runs;
-    a.parts = reinterpret_cast<float*>(b.ws + l.parts);
-  }
-  cudaError_t e = b.type == ATOMO_TYPE_F32 ? sum_type<float>(a, st) : b.type == ATOMO_TYPE_BF16 ? sum_type<__nv_bfloat16>(a, st) : sum_type<__half>(a, st);
-  if (e != cudaSuccess || l.chunks < 2) return (int)e;
-  const int64_t units = (l.chunks - 1) * ((b.cols + 127) / 128);
-  return (int)launch_after(emb_join_kernel, dim3((unsigned)std::min<int64_t>(units, 148 * 4)), dim3(32, kJoinSlices), 0, st, a);
+  a.dout = b.grad; a.ld = b.ld; a.scale = b.scale; a.accumulate = b.accumulate; a.out = b.out; a.ld_out = b.ld_out; a.vec_out = vec_out;
+  a.parts = reinterpret_cast<float*>(b.ws + l.parts); a.ld_part = l.ld_part;
+  e = b.type == ATOMO_TYPE_F32 ? sum_type<float>(a, st) : b.type == ATOMO_TYPE_BF16 ? sum_type<__nv_bfloat16>(a, st) : sum_type<__half>(a, st);
+  if (e != cudaSuccess || l.chunks < 3) return (int)e;           // no run of fewer chunks is long
+  const int64_t units = (l.chunks / 2) * ((b.cols + 127) / 128);
+  return (int)launch_after(emb_join_kernel, dim3((unsigned)std::min<int64_t>(units, 148 * 8)), dim3(32, kJoinSlices), 0, st, a);
 }
 
 }  // namespace atomo

@@ -27,6 +27,13 @@ template <typename T, int V> struct alignas(V * sizeof(T)) Pack { T v[V]; };
 template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_pack(const T* p) { return *reinterpret_cast<const Pack<T, V>*>(p); }
 template <typename T, int V> __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& x) { *reinterpret_cast<Pack<T, V>*>(p) = x; }
 
+// a copy of BYTES bytes (16 or 4) from global to shared memory that the thread waits for with cp.async.wait_group
+template <int BYTES> __device__ __forceinline__ void copy_async(void* shared, const void* global) {
+  const uint32_t s = (uint32_t)__cvta_generic_to_shared(shared);
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(s), "l"(global) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(s), "l"(global), "n"(BYTES) : "memory");
+}
+
 // ---- launches -------------------------------------------------------------------------------------
 // A kernel launched with launch_after() may start while the kernel before it in the stream ends; it calls wait_for_previous() in every
 // thread before it touches memory.
@@ -71,8 +78,9 @@ struct EmbBackward {
   float* out; int64_t ld_out; int accumulate; int32_t* status;
   uint8_t* ws;
 };
+int embedding_configure(int device);                                             // shared memory, cluster size; cudaError_t
 int launch_embedding(const EmbLookup& a, cudaStream_t st);                       // cudaError_t
-uint64_t embedding_workspace(int64_t n, int64_t rows, int64_t cols);
+uint64_t embedding_workspace(int64_t n, int64_t cols);
 int launch_embedding_backward(const EmbBackward& a, cudaStream_t st);            // cudaError_t
 
 // ---- layer norm (atomo_layernorm.cu) --------------------------------------------------------------
