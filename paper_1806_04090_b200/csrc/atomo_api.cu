@@ -406,6 +406,7 @@ int atomo_create(atomo_ctx** out, int device) {
   int e = sp_configure();
   if (e == 0) e = ew_configure();
   if (e == 0) e = embedding_configure(device);
+  if (e == 0) e = layer_norm_configure();
   if (e != 0) return fail_cuda(ctx, (cudaError_t)e, "cudaFuncSetAttribute(max dynamic shared memory)");
   ctx->tc_ok = sp_tc_configure() == 0;
   CK(cudaEventCreateWithFlags(&ctx->ev_fork, cudaEventDisableTiming));

@@ -103,6 +103,11 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {  
   return d;
 }
 
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {                  // a + b, both halves, round to nearest
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {                  // a * b, both halves, round to nearest
   uint64_t d;
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));

@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 #include <string.h>
 
+#include <type_traits>
 #include <vector>
 
 #include "atomo_common.cuh"
@@ -26,6 +27,24 @@ template <> __device__ __forceinline__ __half from_float<__half>(float x) { retu
 template <typename T, int V> struct alignas(V * sizeof(T)) Pack { T v[V]; };
 template <typename T, int V> __device__ __forceinline__ Pack<T, V> load_pack(const T* p) { return *reinterpret_cast<const Pack<T, V>*>(p); }
 template <typename T, int V> __device__ __forceinline__ void store_pack(T* p, const Pack<T, V>& x) { *reinterpret_cast<Pack<T, V>*>(p) = x; }
+
+// two neighbouring values as a pair of fp32, and back
+template <typename T> __device__ __forceinline__ uint64_t pair_of(const T* p) {
+  if constexpr (sizeof(T) == 4) return pack2(p[0], p[1]);
+  else {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return pack2(f.x, f.y);
+  }
+}
+template <typename T> __device__ __forceinline__ void pair_to(T* p, uint64_t v) {
+  float a, b;
+  unpack2(v, a, b);
+  if constexpr (sizeof(T) == 4) { p[0] = a; p[1] = b; }
+  else if constexpr (std::is_same<T, __nv_bfloat16>::value) *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(a, b);
+  else *reinterpret_cast<__half2*>(p) = __floats2half2_rn(a, b);
+}
 
 // a copy of BYTES bytes (16 or 4) from global to shared memory that the thread waits for with cp.async.wait_group
 template <int BYTES> __device__ __forceinline__ void copy_async(void* shared, const void* global) {
@@ -95,6 +114,7 @@ struct NormBackward {
   void* dx; int64_t ld_dx; float *dweight, *dbias;
   float* ws;
 };
+int layer_norm_configure();                                                      // shared memory; cudaError_t
 int launch_layer_norm(const NormForward& a, cudaStream_t st);                    // cudaError_t
 uint64_t layer_norm_workspace(int64_t rows, int64_t cols);
 int launch_layer_norm_backward(const NormBackward& a, cudaStream_t st);          // cudaError_t
