@@ -6,7 +6,8 @@
 // One pass over memory in either direction: a row stays on chip with one group of threads (a warp, or a CTA), each of which owns the
 // same columns in every row that its group takes, so that the weights are loaded once and the sums of dw and db stay in registers
 // too; the groups' sums are then added by a second kernel, in a fixed order.  The rows to come are copied to shared memory meanwhile, by the threads that
-// will use them, so that copies in flight take no registers and are waited for by their own thread alone.  A thread has up to 32 columns, two at a time in packed
+// will use them, so that copies in flight take no registers and are waited for by their own thread alone; rows that are not aligned are copied in whole 16 bytes
+// all the same and shared by the group.  A thread has up to 16 columns, two at a time in packed
 // fp32: what a row costs every warp (shuffles, the exchange among warps) outweighs the arithmetic where a thread has few, and instruction issue then bounds
 // the kernels instead of memory (2048 bf16 columns, 8 per thread: 33 instructions per element forward, 82 us for 32768 rows).
 //   The variance is taken from the values centred on the warp's mean, and the warps' are combined as M2 = sum of M2_w + n_w (mean_w - mean)^2, which takes
@@ -20,20 +21,12 @@ namespace atomo {
 namespace {
 
 constexpr int kGroupMax = 512;                                   // threads per row, at most
-constexpr int kNormCols = kGroupMax * 32;
-constexpr int kWarpsPerCta = 8;                                  // rows side by side where a warp takes a row
+constexpr int kNormCols = kGroupMax * 16;
+constexpr int kCtaThreads = 256;                                 // of a CTA with several groups side by side
 constexpr int kBackCtas = 148 * 4;                               // partial rows of dw and db, at most
-#ifndef FST
-#define FST 4
-#endif
-#ifndef BST
-#define BST 3
-#endif
-// By the bytes of a row that a thread has: rows per step; steps whose rows are in shared memory or on the way there (512 threads with 128 bytes of x and of dy:
-// 128 KB a step)
+// By the bytes of a row that a thread has (up to 64): rows per step; steps whose rows are in shared memory or on the way there
+constexpr int kForwardStages = 4, kBackwardStages = 3;
 __host__ __device__ constexpr int rows_per_step(int bytes) { return bytes <= 32 ? 2 : 1; }
-__host__ __device__ constexpr int forward_stages(int bytes) { return bytes <= 64 ? FST : 2; }
-__host__ __device__ constexpr int backward_stages(int bytes) { return bytes <= 64 ? BST : 1; }
 
 struct Weight { const void* p; int type; };
 __device__ __forceinline__ float weight_at(const Weight& w, int64_t i, float none) {
@@ -47,61 +40,111 @@ __device__ __forceinline__ float weight_at(const Weight& w, int64_t i, float non
 __device__ __forceinline__ uint64_t both(float x) { return pack2(x, x); }
 __device__ __forceinline__ float halves(uint64_t v) { float a, b; unpack2(v, a, b); return a + b; }
 
-// sum over the lanes that differ in the bits below `span`, a power of two
-__device__ __forceinline__ float span_sum(float v, int span) {
-  for (int o = 1; o < span; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+// sum over the lanes that differ in the bits below `span`, a power of two up to CTA / 32
+template <int CTA> __device__ __forceinline__ float span_sum(float v, int span) {
+#pragma unroll
+  for (int o = 1; o < CTA / 32; o <<= 1) if (o < span) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ int warp_span() {                     // warps of the CTA, rounded up to a power of two
-  int span = 1;
-  while (span < (int)(blockDim.x >> 5)) span <<= 1;
-  return span;
+// the threads of a group meet (barrier 0 is the whole CTA's)
+__device__ __forceinline__ void meet(int group, int width) {
+  if (width == 32) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "r"(width) : "memory");
 }
+// this thread's place: the group in its CTA, the thread in its group, the warp whose sums it takes in an exchange (if there is one)
+struct Place {
+  int width, group, lane, span, mate; bool other;
+  __device__ __forceinline__ explicit Place(int width) : width(width), group(threadIdx.x / width), lane(threadIdx.x - group * width), span(1) {
+    while (span * 32 < width) span <<= 1;
+    const int at = threadIdx.x & (span - 1);
+    other = at * 32 < width;
+    mate = group * (width >> 5) + at;
+  }
+};
 __device__ __forceinline__ float one_over_root(float x) {        // to about one unit in the last place
   const float r = rsqrtf(x);
   return fmaf(r * 0.5f, fmaf(-x * r, r, 1.0f), r);
 }
 
-// A thread's packs of the rows that come next: STAGES steps of ROWS rows (of N arrays: x, or x and dy), in shared memory.  16- and 4-byte packs are copied
-// asynchronously; 2-byte ones are loaded.
-template <typename T, int VEC, int PACKS, int ROWS, int STAGES>
-struct RowRing {
-  static constexpr int kBytes = VEC * (int)sizeof(T);
-  static constexpr bool kAsync = kBytes == 16 || kBytes == 4;
-  static constexpr uint32_t kAll = PACKS == 32 ? 0xffffffffu : (1u << (PACKS & 31)) - 1u;
-  Pack<T, VEC>* slot;                  // of this thread
-  __device__ __forceinline__ Pack<T, VEC>* at(int stage, int row, int k) const { return slot + ((stage * ROWS + row) * PACKS + k) * blockDim.x; }
-  __device__ __forceinline__ void put(int stage, int row, int k, const T* p) {
-    if constexpr (kAsync) copy_async<kBytes>(at(stage, row, k), p); else *at(stage, row, k) = load_pack<T, VEC>(p);
+// The rows that come next: STAGES steps of ROWS rows (x, or x and dy by turns) in shared memory, for a group of `width` threads of which this is `lane`.
+// Aligned rows: a thread copies its own packs (of 16 bytes) and waits for nobody else's.  CTA: threads, at most.
+template <typename T, int VEC, int PACKS, int ROWS, int STAGES, int CTA>
+struct OwnRing {
+  static constexpr bool kShared = false;
+  static constexpr uint32_t kAll = (1u << PACKS) - 1u;
+  Pack<T, VEC>* slot; int hop, at; uint32_t in;                  // hop: values between two packs of a thread
+  __device__ __forceinline__ OwnRing(uint4* smem, int, int width, int lane, int, uint32_t in)
+      : slot(reinterpret_cast<Pack<T, VEC>*>(smem) + threadIdx.x), hop(width * VEC), at(lane * VEC), in(in) {}
+  static size_t bytes(int, int) { return (size_t)STAGES * ROWS * PACKS * CTA * 16; }
+  __device__ __forceinline__ void put(int stage, int row, const T* p, const T*, const T*) {
+    p += at;
+    Pack<T, VEC>* to = slot + stage * (ROWS * PACKS * CTA);
+#pragma unroll
+    for (int k = 0; k < PACKS; ++k) if (in >> k & 1u) copy_async<16>(to + (row * PACKS + k) * CTA, p + k * hop);
   }
-  __device__ __forceinline__ void close() { if constexpr (kAsync) asm volatile("cp.async.commit_group;" ::: "memory"); }
-  __device__ __forceinline__ void wait() { if constexpr (kAsync) asm volatile("cp.async.wait_group %0;" :: "n"(STAGES - 1) : "memory"); }
-  // the thread's columns of a row, as pairs; zeros where it has none (in: a bit per pack)
-  __device__ __forceinline__ void get(int stage, int row, uint32_t in, uint64_t (&v)[VEC * PACKS / 2]) const {
-    if (in == kAll) {
+  __device__ __forceinline__ Pack<T, VEC> pack(int stage, int row, int k, uint32_t) const { return slot[stage * (ROWS * PACKS * CTA) + (row * PACKS + k) * CTA]; }
+};
+// Other rows: the group copies the 16 bytes that hold them, as far as they lie within the matrix (its first and last value are given), and all of it waits.
+template <typename T, int VEC, int PACKS, int ROWS, int STAGES, int CTA>
+struct SharedRing {
+  static constexpr bool kShared = true;
+  static constexpr uint32_t kAll = (1u << PACKS) - 1u;
+  uint8_t* base; int width, lane, cols, pitch;
+  static __host__ __device__ __forceinline__ int row_pitch(int cols) { return ((cols * (int)sizeof(T) + 15) / 16 + 1) * 16; }
+  __device__ __forceinline__ SharedRing(uint4* smem, int group, int width, int lane, int cols, uint32_t)
+      : width(width), lane(lane), cols(cols), pitch(row_pitch(cols)) { base = reinterpret_cast<uint8_t*>(smem) + (size_t)group * STAGES * ROWS * pitch; }
+  static size_t bytes(int groups, int cols) { return (size_t)groups * STAGES * ROWS * row_pitch(cols); }
+  __device__ __forceinline__ uint8_t* row_at(int stage, int row) const { return base + (stage * ROWS + row) * pitch; }
+  __device__ __forceinline__ void put(int stage, int row, const T* p, const T* first, const T* last) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15, lo = reinterpret_cast<uintptr_t>(first), hi = reinterpret_cast<uintptr_t>(last + 1);
+    const int n = (int)((reinterpret_cast<uintptr_t>(p + cols) - a + 15) >> 4);
+    uint8_t* to = row_at(stage, row);
+    for (int i = lane; i < n; i += width) {
+      const uintptr_t from = a + (uintptr_t)i * 16;
+      if (from >= lo && from + 16 <= hi) copy_async<16>(to + i * 16, reinterpret_cast<const void*>(from));
+      else {
 #pragma unroll
-      for (int k = 0; k < PACKS; k += VEC > 1 ? 1 : 2) {
-        if constexpr (VEC > 1) {
-          const Pack<T, VEC> raw = *at(stage, row, k);
-#pragma unroll
-          for (int j = 0; j < VEC; j += 2) v[(k * VEC + j) / 2] = pair_of(raw.v + j);
-        } else v[k / 2] = pack2(to_float(at(stage, row, k)->v[0]), to_float(at(stage, row, k + 1)->v[0]));
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < VEC * PACKS / 2; ++e) v[e] = 0;
-#pragma unroll
-      for (int k = 0; k < PACKS; k += VEC > 1 ? 1 : 2) {
-        if (!(in >> k & 1u)) break;                               // (the packs that a thread has are its first ones)
-        if constexpr (VEC > 1) {
-          const Pack<T, VEC> raw = *at(stage, row, k);
-#pragma unroll
-          for (int j = 0; j < VEC; j += 2) v[(k * VEC + j) / 2] = pair_of(raw.v + j);
-        } else v[k / 2] = pack2(to_float(at(stage, row, k)->v[0]), in >> (k + 1) & 1u ? to_float(at(stage, row, k + 1)->v[0]) : 0.0f);
+        for (int j = 0; j < 16; j += (int)sizeof(T))
+          if (from + j >= lo && from + j < hi) *reinterpret_cast<T*>(to + i * 16 + j) = *reinterpret_cast<const T*>(from + j);
       }
     }
   }
+  __device__ __forceinline__ Pack<T, VEC> pack(int stage, int row, int k, uint32_t low) const {
+    return *reinterpret_cast<const Pack<T, VEC>*>(row_at(stage, row) + (low & 15u) + (k * width + lane) * VEC * (int)sizeof(T));
+  }
 };
+template <typename T, int VEC, int PACKS, int ROWS, int STAGES, int CTA>
+using Ring = typename std::conditional<VEC * sizeof(T) == 16, OwnRing<T, VEC, PACKS, ROWS, STAGES, CTA>, SharedRing<T, VEC, PACKS, ROWS, STAGES, CTA>>::type;
+
+// the thread's columns of a row (the low bits of whose address in global memory are given), as pairs; zeros where it has none (in: a bit per pack)
+__device__ __forceinline__ uint32_t low_of(const void* p) { return (uint32_t)reinterpret_cast<uintptr_t>(p); }
+template <typename T, int VEC, int PACKS, typename R>
+__device__ __forceinline__ void get_pairs(const R& ring, int stage, int row, uint32_t low, uint32_t in, uint64_t (&v)[VEC * PACKS / 2]) {
+  if (in == R::kAll) {
+#pragma unroll
+    for (int k = 0; k < PACKS; k += VEC > 1 ? 1 : 2) {
+      if constexpr (VEC > 1) {
+        const Pack<T, VEC> raw = ring.pack(stage, row, k, low);
+#pragma unroll
+        for (int j = 0; j < VEC; j += 2) v[(k * VEC + j) / 2] = pair_of(raw.v + j);
+      } else v[k / 2] = pack2(to_float(ring.pack(stage, row, k, low).v[0]), to_float(ring.pack(stage, row, k + 1, low).v[0]));
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC * PACKS / 2; ++e) v[e] = 0;
+#pragma unroll
+    for (int k = 0; k < PACKS; k += VEC > 1 ? 1 : 2) {
+      if (!(in >> k & 1u)) break;                                 // (the packs that a thread has are its first ones)
+      if constexpr (VEC > 1) {
+        const Pack<T, VEC> raw = ring.pack(stage, row, k, low);
+#pragma unroll
+        for (int j = 0; j < VEC; j += 2) v[(k * VEC + j) / 2] = pair_of(raw.v + j);
+      } else v[k / 2] = pack2(to_float(ring.pack(stage, row, k, low).v[0]), in >> (k + 1) & 1u ? to_float(ring.pack(stage, row, k + 1, low).v[0]) : 0.0f);
+    }
+  }
+}
+__device__ __forceinline__ void close_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
 template <typename T, int VEC, int PACKS>
 __device__ __forceinline__ void put_pairs(T* row, int width, int lane, uint32_t in, const uint64_t (&v)[VEC * PACKS / 2]) {
   if constexpr (VEC > 1) {
@@ -148,57 +191,55 @@ __device__ __forceinline__ void get_weight(const Weight& w, int width, int lane,
   for (int e = 0; e < VEC * PACKS / 2; ++e) v[e] = pack2(f[2 * e], f[2 * e + 1]);
 }
 
-// Columns of a thread: PACKS pieces of VEC neighbouring ones, a group's width apart; with 32 the weights are read anew for every row.
-template <typename T, int VEC, int PACKS, bool WARP>
-__global__ void __launch_bounds__(WARP ? kWarpsPerCta * 32 : kGroupMax) ln_forward_kernel(const T* x, int64_t rows, int cols, int64_t ld, Weight weight, Weight bias,
-                                                                                         float eps, T* y, int64_t ld_y, float* __restrict__ mean, float* __restrict__ rstd) {
-  constexpr int E = VEC * PACKS, R = rows_per_step(E * sizeof(T)), kStages = forward_stages(E * sizeof(T));
-  constexpr bool kKeep = E < 32;
+// Columns of a thread: PACKS pieces of VEC neighbouring ones, a group's width apart.
+template <typename T, int VEC, int PACKS, int CTA>
+__global__ void __launch_bounds__(CTA, 512 / CTA) ln_forward_kernel(int group_width, const T* x, int64_t rows, int cols, int64_t ld, Weight weight, Weight bias,
+                                                               float eps, T* y, int64_t ld_y, float* __restrict__ mean, float* __restrict__ rstd) {
+  constexpr int E = VEC * PACKS, R = rows_per_step(E * sizeof(T)), kStages = kForwardStages;
   extern __shared__ uint4 s_ring[];
   __shared__ float2 s_sum[2][R][16];
   __shared__ float s_count[16];
-  const int width = WARP ? 32 : blockDim.x, lane = WARP ? threadIdx.x & 31 : threadIdx.x, warps = blockDim.x >> 5;
-  const int64_t groups = WARP ? (int64_t)gridDim.x * kWarpsPerCta : gridDim.x;
-  const int64_t group = WARP ? (int64_t)blockIdx.x * kWarpsPerCta + (threadIdx.x >> 5) : blockIdx.x;
+  const Place at(group_width);
+  const int width = at.width, lane = at.lane, beside = blockDim.x / width;
+  const int ahead = gridDim.x * beside * R, first = ((int)blockIdx.x * beside + at.group) * R;        // rows between two steps; the first one
   const float inv = 1.0f / (float)cols;
   uint32_t in = 0;                                               // packs that lie inside the row
 #pragma unroll
   for (int k = 0; k < PACKS; ++k) if ((k * width + lane) * VEC < cols) in |= 1u << k;
-  const bool full = in == RowRing<T, VEC, PACKS, R, kStages>::kAll;
-  RowRing<T, VEC, PACKS, R, kStages> ring{reinterpret_cast<Pack<T, VEC>*>(s_ring) + threadIdx.x};
-  const T* from = x + group * R * ld + lane * VEC;               // the next row to fetch
-  int64_t fetched = group * R;
+  using Rows = Ring<T, VEC, PACKS, R, kStages, CTA>;
+  const bool full = in == Rows::kAll;
+  Rows ring(s_ring, at.group, width, lane, cols, in);
+  const int64_t step = ahead * ld, step_y = ahead * ld_y;
+  const T *from = x + first * ld, *last = x + (rows - 1) * ld + cols - 1;          // the next rows to fetch; the matrix's last value
+  int left = (int)rows - first;                                  // rows from there on
   auto fetch = [&](int stage) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-#pragma unroll
-      for (int k = 0; k < PACKS; ++k) if (fetched + r < rows && (in >> k & 1u)) ring.put(stage, r, k, from + r * ld + k * width * VEC);
-    }
-    ring.close();
-    from += groups * R * ld; fetched += groups * R;
+    for (int r = 0; r < R; ++r) if (r < left) ring.put(stage, r, from + r * ld, x, last);
+    close_copies();
+    from += step; left -= ahead;
   };
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) fetch(i);
   uint64_t w[E / 2], b[E / 2];
-  if constexpr (kKeep) { get_weight<VEC, PACKS>(weight, width, lane, in, 1.0f, w); get_weight<VEC, PACKS>(bias, width, lane, in, 0.0f, b); }
+  get_weight<VEC, PACKS>(weight, width, lane, in, 1.0f, w);
+  get_weight<VEC, PACKS>(bias, width, lane, in, 0.0f, b);
   const float count = warp_sum((float)(__popc(in) * VEC)), inv_count = 1.0f / count;       // columns of this warp
-  const int span = WARP ? 1 : warp_span(), mate = threadIdx.x & (span - 1);
-  const bool other = mate < warps;
   float mate_count = 0.0f, mate_inv = 0.0f;                      // columns of the warp whose sums this lane takes
-  if constexpr (!WARP) {
-    if ((threadIdx.x & 31) == 0) s_count[threadIdx.x >> 5] = count;
-    __syncthreads();
-    if (other) { mate_count = s_count[mate]; mate_inv = 1.0f / mate_count; }
-  }
+  if ((threadIdx.x & 31) == 0) s_count[threadIdx.x >> 5] = count;
+  __syncthreads();
+  if (at.other) { mate_count = s_count[at.mate]; mate_inv = 1.0f / mate_count; }
   int stage = 0, turn = 0;
-  for (int64_t r0 = group * R; r0 < rows; r0 += groups * R, turn ^= 1) {
+  uint32_t low = low_of(x + first * ld);
+  T* to = y + first * ld_y;
+  for (int r0 = first; r0 < (int)rows; r0 += ahead, turn ^= 1) {
+    if constexpr (Rows::kShared) { wait_copies<kStages - 2>(); meet(at.group, width); }       // the copies of the whole group; nobody reads the step before any more
     fetch(stage == 0 ? kStages - 1 : stage - 1);
-    ring.wait();
+    if constexpr (!Rows::kShared) wait_copies<kStages - 1>();
     uint64_t v[R][E / 2];
     float mu[R], var[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if (r0 + r < rows) ring.get(stage, r, in, v[r]);
+      if (r0 + r < (int)rows) get_pairs<T, VEC, PACKS>(ring, stage, r, low + r * (uint32_t)ld * (uint32_t)sizeof(T), in, v[r]);
       else {
 #pragma unroll
         for (int e = 0; e < E / 2; ++e) v[r][e] = 0;
@@ -231,98 +272,94 @@ __global__ void __launch_bounds__(WARP ? kWarpsPerCta * 32 : kGroupMax) ln_forwa
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) var[r] = warp_sum(var[r]);
-    if constexpr (!WARP) {
+    if (width > 32) {
       if ((threadIdx.x & 31) == 0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) s_sum[turn][r][threadIdx.x >> 5] = make_float2(mu[r], var[r]);
       }
-      __syncthreads();
+      meet(at.group, width);
 #pragma unroll
       for (int r = 0; r < R; ++r) {                               // a lane per warp
-        const float2 q = other ? s_sum[turn][r][mate] : make_float2(0.0f, 0.0f);
-        mu[r] = span_sum(q.x, span);
+        const float2 q = at.other ? s_sum[turn][r][at.mate] : make_float2(0.0f, 0.0f);
+        mu[r] = span_sum<CTA>(q.x, at.span);
         const float d = fmaf(-mu[r], inv, q.x * mate_inv);
-        var[r] = span_sum(fmaf(mate_count * d, d, q.y), span);
+        var[r] = span_sum<CTA>(fmaf(mate_count * d, d, q.y), at.span);
       }
     }
-    if constexpr (!kKeep) { get_weight<VEC, PACKS>(weight, width, lane, in, 1.0f, w); get_weight<VEC, PACKS>(bias, width, lane, in, 0.0f, b); }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if (r0 + r < rows) {
+      if (r0 + r < (int)rows) {
         const float m = mu[r] * inv, rs = one_over_root(fmaf(var[r], inv, eps));
         const uint64_t centre = both(-m), scale = both(rs);
 #pragma unroll
         for (int e = 0; e < E / 2; ++e) v[r][e] = fma2(mul2(add2(v[r][e], centre), scale), w[e], b[e]);
-        put_pairs<T, VEC, PACKS>(y + (r0 + r) * ld_y, width, lane, in, v[r]);
+        put_pairs<T, VEC, PACKS>(to + r * ld_y, width, lane, in, v[r]);
         if (lane == 0) { mean[r0 + r] = m; rstd[r0 + r] = rs; }
       }
     }
     stage = stage + 1 == kStages ? 0 : stage + 1;
+    low += (uint32_t)step * (uint32_t)sizeof(T); to += step_y;
   }
 }
 
-template <typename T, int VEC, int PACKS, bool WARP>
-__global__ void __launch_bounds__(WARP ? kWarpsPerCta * 32 : kGroupMax) ln_backward_kernel(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, int64_t rows, int cols,
-                                                                                          Weight weight, const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                                                          T* dx, int64_t ld_dx, float* __restrict__ parts) {
-  constexpr int E = VEC * PACKS, R = rows_per_step(E * sizeof(T)), kStages = backward_stages(E * sizeof(T));
-  constexpr bool kKeep = E < 32;
-  extern __shared__ uint4 s_ring[];                              // WARP: afterwards [warps][2][cols] floats
+template <typename T, int VEC, int PACKS, int CTA>
+__global__ void __launch_bounds__(CTA, 512 / CTA) ln_backward_kernel(int group_width, const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, int64_t rows, int cols,
+                                                                Weight weight, const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                                T* dx, int64_t ld_dx, float* __restrict__ parts) {
+  constexpr int E = VEC * PACKS, R = rows_per_step(E * sizeof(T)), kStages = kBackwardStages;
+  extern __shared__ uint4 s_ring[];                              // afterwards, of several groups: [groups][2][cols] floats
   __shared__ float2 s_sum[2][R][16];
-  const int width = WARP ? 32 : blockDim.x, lane = WARP ? threadIdx.x & 31 : threadIdx.x;
-  const int64_t groups = WARP ? (int64_t)gridDim.x * kWarpsPerCta : gridDim.x;
-  const int64_t group = WARP ? (int64_t)blockIdx.x * kWarpsPerCta + (threadIdx.x >> 5) : blockIdx.x;
+  const Place at(group_width);
+  const int width = at.width, lane = at.lane, beside = blockDim.x / width;
+  const int ahead = gridDim.x * beside * R, first = ((int)blockIdx.x * beside + at.group) * R;        // rows between two steps; the first one
   const float inv = 1.0f / (float)cols;
   uint32_t in = 0;                                               // packs that lie inside the row
 #pragma unroll
   for (int k = 0; k < PACKS; ++k) if ((k * width + lane) * VEC < cols) in |= 1u << k;
-  RowRing<T, VEC, PACKS, 2 * R, kStages> ring{reinterpret_cast<Pack<T, VEC>*>(s_ring) + threadIdx.x};
-  const T *from_x = x + group * R * ld_x + lane * VEC, *from_dy = dy + group * R * ld_dy + lane * VEC;       // the next row to fetch
-  int64_t fetched = group * R;
+  using Rows = Ring<T, VEC, PACKS, 2 * R, kStages, CTA>;
+  Rows ring(s_ring, at.group, width, lane, cols, in);
+  const int64_t step_x = ahead * ld_x, step_dy = ahead * ld_dy, step_dx = ahead * ld_dx;
+  const T *from_x = x + first * ld_x, *from_dy = dy + first * ld_dy;               // the next rows to fetch
+  const T *last_x = x + (rows - 1) * ld_x + cols - 1, *last_dy = dy + (rows - 1) * ld_dy + cols - 1;
+  int left = (int)rows - first;                                  // rows from there on
   auto fetch = [&](int stage) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-#pragma unroll
-      for (int k = 0; k < PACKS; ++k) {
-        if (fetched + r < rows && (in >> k & 1u)) {
-          ring.put(stage, 2 * r, k, from_x + r * ld_x + k * width * VEC);
-          ring.put(stage, 2 * r + 1, k, from_dy + r * ld_dy + k * width * VEC);
-        }
-      }
-    }
-    ring.close();
-    from_x += groups * R * ld_x; from_dy += groups * R * ld_dy; fetched += groups * R;
+    for (int r = 0; r < R; ++r)
+      if (r < left) { ring.put(stage, 2 * r, from_x + r * ld_x, x, last_x); ring.put(stage, 2 * r + 1, from_dy + r * ld_dy, dy, last_dy); }
+    close_copies();
+    from_x += step_x; from_dy += step_dy; left -= ahead;
   };
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) fetch(i);
   uint64_t w[E / 2], dw[E / 2], db[E / 2];
-  if constexpr (kKeep) get_weight<VEC, PACKS>(weight, width, lane, in, 1.0f, w);
+  get_weight<VEC, PACKS>(weight, width, lane, in, 1.0f, w);
 #pragma unroll
   for (int e = 0; e < E / 2; ++e) { dw[e] = 0; db[e] = 0; }
-  const int span = WARP ? 1 : warp_span(), mate = threadIdx.x & (span - 1);
-  const bool other = mate < (int)(blockDim.x >> 5);
   int stage = 0, turn = 0;
   float next_mu[R], next_rs[R];
-  auto stats = [&](int64_t r0) {
+  auto stats = [&](int r0) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) { next_mu[r] = r0 + r < rows ? mean[r0 + r] : 0.0f; next_rs[r] = r0 + r < rows ? rstd[r0 + r] : 0.0f; }
+    for (int r = 0; r < R; ++r) { next_mu[r] = r0 + r < (int)rows ? mean[r0 + r] : 0.0f; next_rs[r] = r0 + r < (int)rows ? rstd[r0 + r] : 0.0f; }
   };
-  stats(group * R);
-  for (int64_t r0 = group * R; r0 < rows; r0 += groups * R, turn ^= 1) {
+  stats(first);
+  uint32_t low_x = low_of(x + first * ld_x), low_dy = low_of(dy + first * ld_dy);
+  T* to = dx + first * ld_dx;
+  for (int r0 = first; r0 < (int)rows; r0 += ahead, turn ^= 1) {
     float mu[R], rs[R];
     float2 s[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) { mu[r] = next_mu[r]; rs[r] = next_rs[r]; }
-    stats(r0 + groups * R);
+    stats(r0 + ahead);
+    if constexpr (Rows::kShared) { wait_copies<kStages - 2>(); meet(at.group, width); }
     fetch(stage == 0 ? kStages - 1 : stage - 1);
-    ring.wait();
-    if constexpr (!kKeep) get_weight<VEC, PACKS>(weight, width, lane, in, 1.0f, w);
+    if constexpr (!Rows::kShared) wait_copies<kStages - 1>();
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       s[r] = make_float2(0.0f, 0.0f);
-      if (r0 + r >= rows) continue;
+      if (r0 + r >= (int)rows) continue;
       uint64_t h[E / 2], d[E / 2], s1 = 0, s2 = 0;
-      ring.get(stage, 2 * r, in, h); ring.get(stage, 2 * r + 1, in, d);            // (a column without a value has d = 0 and counts for nothing)
+      get_pairs<T, VEC, PACKS>(ring, stage, 2 * r, low_x + r * (uint32_t)ld_x * (uint32_t)sizeof(T), in, h);
+      get_pairs<T, VEC, PACKS>(ring, stage, 2 * r + 1, low_dy + r * (uint32_t)ld_dy * (uint32_t)sizeof(T), in, d);            // (a column without a value has d = 0 and counts for nothing)
       const uint64_t centre = both(-mu[r]), scale = both(rs[r]);
 #pragma unroll
       for (int e = 0; e < E / 2; ++e) {
@@ -334,50 +371,51 @@ __global__ void __launch_bounds__(WARP ? kWarpsPerCta * 32 : kGroupMax) ln_backw
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) { s[r].x = warp_sum(s[r].x); s[r].y = warp_sum(s[r].y); }
-    if constexpr (!WARP) {
+    if (width > 32) {
       if ((threadIdx.x & 31) == 0) {
 #pragma unroll
         for (int r = 0; r < R; ++r) s_sum[turn][r][threadIdx.x >> 5] = s[r];
       }
-      __syncthreads();
+      meet(at.group, width);
 #pragma unroll
       for (int r = 0; r < R; ++r) {                               // a lane per warp
-        const float2 q = other ? s_sum[turn][r][mate] : make_float2(0.0f, 0.0f);
-        s[r] = make_float2(span_sum(q.x, span), span_sum(q.y, span));
+        const float2 q = at.other ? s_sum[turn][r][at.mate] : make_float2(0.0f, 0.0f);
+        s[r] = make_float2(span_sum<CTA>(q.x, at.span), span_sum<CTA>(q.y, at.span));
       }
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if (r0 + r < rows) {
+      if (r0 + r < (int)rows) {
         // rs (u - m1 - hat m2)
         const uint64_t centre = both(-mu[r]), scale = both(rs[r]), m1 = both(-rs[r] * (s[r].x * inv)), m2 = both(-rs[r] * (s[r].y * inv));
         uint64_t h[E / 2], d[E / 2];
-        ring.get(stage, 2 * r, in, h); ring.get(stage, 2 * r + 1, in, d);          // again, rather than kept in registers
+        get_pairs<T, VEC, PACKS>(ring, stage, 2 * r, low_x + r * (uint32_t)ld_x * (uint32_t)sizeof(T), in, h);
+        get_pairs<T, VEC, PACKS>(ring, stage, 2 * r + 1, low_dy + r * (uint32_t)ld_dy * (uint32_t)sizeof(T), in, d);          // again, rather than kept in registers
 #pragma unroll
         for (int e = 0; e < E / 2; ++e) {
           const uint64_t hat = mul2(add2(h[e], centre), scale), u = mul2(d[e], w[e]);
           d[e] = fma2(hat, m2, fma2(u, scale, m1));
         }
-        put_pairs<T, VEC, PACKS>(dx + (r0 + r) * ld_dx, width, lane, in, d);
+        put_pairs<T, VEC, PACKS>(to + r * ld_dx, width, lane, in, d);
       }
     }
     stage = stage + 1 == kStages ? 0 : stage + 1;
+    low_x += (uint32_t)step_x * (uint32_t)sizeof(T); low_dy += (uint32_t)step_dy * (uint32_t)sizeof(T); to += step_dx;
   }
   // this CTA's rows of partial sums: dw, then db
   float* part_w = parts + (int64_t)blockIdx.x * cols;
   float* part_b = parts + ((int64_t)gridDim.x + blockIdx.x) * cols;
-  if constexpr (WARP) {
+  if (beside > 1) {
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();                                             // the ring is no longer read
     float* s_cols = reinterpret_cast<float*>(s_ring);
-    float* mine = s_cols + (threadIdx.x >> 5) * 2 * cols;
+    float* mine = s_cols + at.group * 2 * cols;
     put_columns<VEC, PACKS>(mine, width, lane, in, dw);
     put_columns<VEC, PACKS>(mine + cols, width, lane, in, db);
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) {
       float t = 0.0f;
-#pragma unroll
-      for (int v = 0; v < kWarpsPerCta; ++v) t += s_cols[v * 2 * cols + c];
+      for (int v = 0; v < beside; ++v) t += s_cols[v * 2 * cols + c];
       if (c < cols) part_w[c] = t; else part_b[c - cols] = t;
     }
   } else {
@@ -408,7 +446,7 @@ __global__ void __launch_bounds__(32 * kJoinRows) ln_join_kernel(const float* __
 }
 
 // ---- rows longer than the registers hold ----------------------------------------------------------
-constexpr int kLongThreads = 1024;
+constexpr int kLongThreads = 512;
 // sums of R values over the CTA (which meets once; s: R x 32 floats that nobody reads any more)
 template <int R>
 __device__ __forceinline__ void long_sum(float (&v)[R], float* s) {
@@ -416,59 +454,90 @@ __device__ __forceinline__ void long_sum(float (&v)[R], float* s) {
   for (int r = 0; r < R; ++r) { v[r] = warp_sum(v[r]); if ((threadIdx.x & 31) == 0) s[r * 32 + (threadIdx.x >> 5)] = v[r]; }
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < R; ++r) v[r] = warp_sum(s[r * 32 + (threadIdx.x & 31)]);
+  for (int r = 0; r < R; ++r) v[r] = warp_sum((threadIdx.x & 31) < kLongThreads / 32 ? s[r * 32 + (threadIdx.x & 31)] : 0.0f);
 }
-template <typename T>
-__global__ void __launch_bounds__(kLongThreads) ln_forward_long_kernel(const T* x, int cols, int64_t ld, Weight weight, Weight bias, float eps,
-                                                                       T* y, int64_t ld_y, float* __restrict__ mean, float* __restrict__ rstd) {
+// (VEC columns at a time: 16 bytes where the rows allow it)
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kLongThreads) ln_forward_long_kernel(const T* x, int cols, int64_t ld, Weight weight, Weight bias, float eps, T* y, int64_t ld_y, float* mean, float* rstd) {
   __shared__ float s_sum[2][32];
   const int64_t row = blockIdx.x;
   const T* p = x + row * ld;
   float v[1] = {0.0f};
-  for (int c = threadIdx.x; c < cols; c += kLongThreads) v[0] += to_float(p[c]);
+#pragma unroll 4
+  for (int c = threadIdx.x * VEC; c < cols; c += kLongThreads * VEC) {
+    const Pack<T, VEC> q = load_pack<T, VEC>(p + c);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) v[0] += to_float(q.v[j]);
+  }
   long_sum<1>(v, s_sum[0]);
   const float mu = v[0] / (float)cols;
   v[0] = 0.0f;
-  for (int c = threadIdx.x; c < cols; c += kLongThreads) { const float d = to_float(p[c]) - mu; v[0] = fmaf(d, d, v[0]); }
+#pragma unroll 4
+  for (int c = threadIdx.x * VEC; c < cols; c += kLongThreads * VEC) {
+    const Pack<T, VEC> q = load_pack<T, VEC>(p + c);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) { const float d = to_float(q.v[j]) - mu; v[0] = fmaf(d, d, v[0]); }
+  }
   long_sum<1>(v, s_sum[1]);
-  const float rs = 1.0f / sqrtf(v[0] / (float)cols + eps);
-  for (int c = threadIdx.x; c < cols; c += kLongThreads)
-    y[row * ld_y + c] = from_float<T>(fmaf((to_float(p[c]) - mu) * rs, weight_at(weight, c, 1.0f), weight_at(bias, c, 0.0f)));
+  const float rs = one_over_root(v[0] / (float)cols + eps);
+#pragma unroll 2
+  for (int c = threadIdx.x * VEC; c < cols; c += kLongThreads * VEC) {
+    Pack<T, VEC> q = load_pack<T, VEC>(p + c);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) q.v[j] = from_float<T>(fmaf((to_float(q.v[j]) - mu) * rs, weight_at(weight, c + j, 1.0f), weight_at(bias, c + j, 0.0f)));
+    store_pack<T, VEC>(y + row * ld_y + c, q);
+  }
   if (threadIdx.x == 0) { mean[row] = mu; rstd[row] = rs; }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kLongThreads) ln_backward_long_kernel(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, int cols, Weight weight,
-                                                                        const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, int64_t ld_dx) {
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kLongThreads) ln_backward_long_kernel(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, int cols, Weight weight, const float* mean, const float* rstd,
+                                                                        T* dx, int64_t ld_dx) {
   __shared__ float s_sum[2 * 32];
   const int64_t row = blockIdx.x;
   const float mu = mean[row], rs = rstd[row];
   float s[2] = {0.0f, 0.0f};
-  for (int c = threadIdx.x; c < cols; c += kLongThreads) {
-    const float u = to_float(dy[row * ld_dy + c]) * weight_at(weight, c, 1.0f), hat = (to_float(x[row * ld_x + c]) - mu) * rs;
-    s[0] += u; s[1] = fmaf(u, hat, s[1]);
+#pragma unroll 2
+  for (int c = threadIdx.x * VEC; c < cols; c += kLongThreads * VEC) {
+    const Pack<T, VEC> d = load_pack<T, VEC>(dy + row * ld_dy + c), q = load_pack<T, VEC>(x + row * ld_x + c);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const float u = to_float(d.v[j]) * weight_at(weight, c + j, 1.0f), hat = (to_float(q.v[j]) - mu) * rs;
+      s[0] += u; s[1] = fmaf(u, hat, s[1]);
+    }
   }
   long_sum<2>(s, s_sum);
   const float m1 = s[0] / (float)cols, m2 = s[1] / (float)cols;
-  for (int c = threadIdx.x; c < cols; c += kLongThreads) {
-    const float u = to_float(dy[row * ld_dy + c]) * weight_at(weight, c, 1.0f), hat = (to_float(x[row * ld_x + c]) - mu) * rs;
-    dx[row * ld_dx + c] = from_float<T>(rs * (u - m1 - hat * m2));
+#pragma unroll 2
+  for (int c = threadIdx.x * VEC; c < cols; c += kLongThreads * VEC) {
+    Pack<T, VEC> d = load_pack<T, VEC>(dy + row * ld_dy + c);
+    const Pack<T, VEC> q = load_pack<T, VEC>(x + row * ld_x + c);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const float u = to_float(d.v[j]) * weight_at(weight, c + j, 1.0f), hat = (to_float(q.v[j]) - mu) * rs;
+      d.v[j] = from_float<T>(rs * (u - m1 - hat * m2));
+    }
+    store_pack<T, VEC>(dx + row * ld_dx + c, d);
   }
 }
-// partial sums of dw and db: a CTA takes 256 columns of every gridDim.y-th row
-template <typename T>
-__global__ void __launch_bounds__(256) ln_columns_kernel(const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, int64_t rows, int cols,
+// partial sums of dw and db: a CTA takes 256 VEC columns of every gridDim.y-th row
+template <typename T, int VEC>
+__global__ void __launch_bounds__(256) ln_columns_kernel(const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ x, int64_t ld_x, int64_t rows, int cols,
                                                          const float* __restrict__ mean, const float* __restrict__ rstd, float* __restrict__ parts) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * VEC;
   if (c >= cols) return;
-  float w = 0.0f, b = 0.0f;
+  float w[VEC], b[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) { w[j] = 0.0f; b[j] = 0.0f; }
 #pragma unroll 4
   for (int64_t r = blockIdx.y; r < rows; r += gridDim.y) {
-    const float d = to_float(dy[r * ld_dy + c]);
-    w = fmaf(d, (to_float(x[r * ld_x + c]) - mean[r]) * rstd[r], w); b += d;
+    const Pack<T, VEC> d = load_pack<T, VEC>(dy + r * ld_dy + c), q = load_pack<T, VEC>(x + r * ld_x + c);
+    const float mu = mean[r], rs = rstd[r];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) { w[j] = fmaf(to_float(d.v[j]), (to_float(q.v[j]) - mu) * rs, w[j]); b[j] += to_float(d.v[j]); }
   }
-  parts[(int64_t)blockIdx.y * cols + c] = w;
-  parts[((int64_t)gridDim.y + blockIdx.y) * cols + c] = b;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) { parts[(int64_t)blockIdx.y * cols + c + j] = w[j]; parts[((int64_t)gridDim.y + blockIdx.y) * cols + c + j] = b[j]; }
 }
 
 // ---- choice of form -------------------------------------------------------------------------------
@@ -479,51 +548,63 @@ int pack_bytes(const void* p, int64_t ld, int64_t cols, int size) {
   return size;
 }
 template <int VEC, int PACKS> struct Form { static constexpr int kVec = VEC, kPacks = PACKS; };
-// Columns per thread: one pack where a warp then holds the row, else 16 (a warp up to 512 columns, CTAs of up to 512 threads from there), else 32.
+// Columns per thread: one pack where a warp then holds the row, else 16 (a warp up to 512 columns, CTAs of up to 512 threads from there).
 template <typename T, int VEC, typename F> cudaError_t by_packs(int64_t cols, F f) {
   constexpr int kFew = VEC >= 4 ? VEC : 4;
   if (cols <= 32 * kFew) return f(Form<VEC, kFew / VEC>{});
-  return cols <= kGroupMax * 16 ? f(Form<VEC, 16 / VEC>{}) : f(Form<VEC, 32 / VEC>{});
+  return f(Form<VEC, 16 / VEC>{});
 }
 template <typename T, typename F> cudaError_t by_form(int bytes, int64_t cols, F f) {
   if (bytes == 16) return by_packs<T, 16 / (int)sizeof(T)>(cols, f);
   if constexpr (sizeof(T) == 2) { if (bytes == 4) return by_packs<T, 2>(cols, f); }
   return by_packs<T, 1>(cols, f);
 }
-// CTAs of a kernel that the GPU holds at a time, asked for once per number of warps (`known`: 0 before that)
+// CTAs of a kernel that the GPU holds at a time.  What its registers allow is asked for once per number of warps (`known`: 0 before that); then what shared
+// memory does, 227 KB of it with 1 KB for each CTA and what it has besides the ring.
 int resident(const void* kernel, int threads, size_t smem, int (&known)[17]) {
   int& n = known[threads / 32];
   if (n == 0) {
     int per = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, threads, smem) != cudaSuccess) cudaGetLastError();
-    n = 148 * std::max(per, 1);
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, threads, 0) != cudaSuccess) cudaGetLastError();
+    n = std::max(per, 1);
   }
-  return n;
+  return 148 * std::max(1, std::min(n, (int)(227 * 1024 / (smem + 2048))));
 }
 
+// threads of a group, of a CTA
+struct Shape { int width, threads; };
+template <int COLUMNS> Shape shape_of(int64_t cols) {
+  const int width = (int)((cols + 32 * COLUMNS - 1) / (32 * COLUMNS)) * 32;
+  return Shape{width, width <= kCtaThreads ? kCtaThreads / width * width : width};
+}
+
+template <typename T, int VEC, int PACKS, int CTA>
+cudaError_t forward_cta(const NormForward& a, Shape s, cudaStream_t st) {
+  constexpr int R = rows_per_step(VEC * PACKS * (int)sizeof(T));
+  const int64_t step = (int64_t)s.threads / s.width * R;         // rows of a CTA's step
+  const size_t smem = Ring<T, VEC, PACKS, R, kForwardStages, CTA>::bytes(s.threads / s.width, (int)a.cols);
+  static int known[17];
+  const int grid = (int)std::min<int64_t>((a.rows + step - 1) / step, resident((const void*)ln_forward_kernel<T, VEC, PACKS, CTA>, s.threads, smem, known));
+  ln_forward_kernel<T, VEC, PACKS, CTA><<<grid, s.threads, smem, st>>>(s.width, (const T*)a.x, a.rows, (int)a.cols, a.ld, Weight{a.weight, a.weight_type}, Weight{a.bias, a.weight_type}, a.eps,
+                                                                       (T*)a.y, a.ld_y, a.mean, a.rstd);
+  return cudaGetLastError();
+}
 template <typename T, int VEC, int PACKS>
 cudaError_t forward_form(const NormForward& a, cudaStream_t st) {
-  constexpr int kBytes = VEC * PACKS * (int)sizeof(T), R = rows_per_step(kBytes);
-  const Weight w{a.weight, a.weight_type}, b{a.bias, a.weight_type};
-  const bool warp = a.cols <= 32 * VEC * PACKS;
-  const int threads = warp ? kWarpsPerCta * 32 : (int)((a.cols + 32 * VEC * PACKS - 1) / (32 * VEC * PACKS)) * 32;
-  const int64_t step = warp ? kWarpsPerCta * R : R;
-  const size_t smem = (size_t)forward_stages(kBytes) * R * threads * kBytes;
-  static int known[2][17];
-  const void* kernel = warp ? (const void*)ln_forward_kernel<T, VEC, PACKS, true> : (const void*)ln_forward_kernel<T, VEC, PACKS, false>;
-  const int grid = (int)std::min<int64_t>((a.rows + step - 1) / step, resident(kernel, threads, smem, known[warp]));
-  if (warp) ln_forward_kernel<T, VEC, PACKS, true><<<grid, threads, smem, st>>>((const T*)a.x, a.rows, (int)a.cols, a.ld, w, b, a.eps, (T*)a.y, a.ld_y, a.mean, a.rstd);
-  else ln_forward_kernel<T, VEC, PACKS, false><<<grid, threads, smem, st>>>((const T*)a.x, a.rows, (int)a.cols, a.ld, w, b, a.eps, (T*)a.y, a.ld_y, a.mean, a.rstd);
-  return cudaGetLastError();
+  const Shape s = shape_of<VEC * PACKS>(a.cols);
+  if constexpr (VEC * PACKS == 16) { if (s.threads > kCtaThreads) return forward_cta<T, VEC, PACKS, kGroupMax>(a, s, st); }
+  return forward_cta<T, VEC, PACKS, kCtaThreads>(a, s, st);
 }
 template <typename T>
 cudaError_t forward_type(const NormForward& a, cudaStream_t st) {
+  const int bytes = std::min(pack_bytes(a.x, a.ld, a.cols, sizeof(T)), pack_bytes(a.y, a.ld_y, a.cols, sizeof(T)));
   if (a.cols > kNormCols) {
-    ln_forward_long_kernel<T><<<(unsigned)a.rows, kLongThreads, 0, st>>>((const T*)a.x, (int)a.cols, a.ld, Weight{a.weight, a.weight_type}, Weight{a.bias, a.weight_type}, a.eps,
-                                                                        (T*)a.y, a.ld_y, a.mean, a.rstd);
+    auto launch = [&](auto kernel) {
+      kernel<<<(unsigned)a.rows, kLongThreads, 0, st>>>((const T*)a.x, (int)a.cols, a.ld, Weight{a.weight, a.weight_type}, Weight{a.bias, a.weight_type}, a.eps, (T*)a.y, a.ld_y, a.mean, a.rstd);
+    };
+    if (bytes == 16) launch(ln_forward_long_kernel<T, 16 / sizeof(T)>); else launch(ln_forward_long_kernel<T, 1>);
     return cudaGetLastError();
   }
-  const int bytes = std::min(pack_bytes(a.x, a.ld, a.cols, sizeof(T)), pack_bytes(a.y, a.ld_y, a.cols, sizeof(T)));
   return by_form<T>(bytes, a.cols, [&](auto f) { return forward_form<T, decltype(f)::kVec, decltype(f)::kPacks>(a, st); });
 }
 
@@ -533,35 +614,39 @@ cudaError_t backward_join(const NormBackward& a, int n, cudaStream_t st) {
   if (!a.dweight && !a.dbias) return cudaSuccess;
   return launch_after(ln_join_kernel, dim3((unsigned)((a.cols + 31) / 32), 2), dim3(32, kJoinRows), 0, st, a.ws, n, (int)a.cols, a.dweight, a.dbias);
 }
-template <typename T, int VEC, int PACKS>
-cudaError_t backward_form(const NormBackward& a, cudaStream_t st) {
-  constexpr int kBytes = VEC * PACKS * (int)sizeof(T), R = rows_per_step(kBytes);
-  const Weight w{a.weight, a.weight_type};
-  const bool warp = a.cols <= 32 * VEC * PACKS;
-  const int threads = warp ? kWarpsPerCta * 32 : (int)((a.cols + 32 * VEC * PACKS - 1) / (32 * VEC * PACKS)) * 32;
-  const int64_t step = warp ? kWarpsPerCta * R : R;
-  const size_t ring = (size_t)backward_stages(kBytes) * 2 * R * threads * kBytes;
-  const size_t smem = warp ? std::max<size_t>(ring, (size_t)kWarpsPerCta * 2 * a.cols * 4) : ring;
-  static int known[2][17];
-  const void* kernel = warp ? (const void*)ln_backward_kernel<T, VEC, PACKS, true> : (const void*)ln_backward_kernel<T, VEC, PACKS, false>;
-  const int grid = (int)std::min<int64_t>(back_ctas(a.rows, step), warp ? 148 * 2 : resident(kernel, threads, smem, known[warp]));
-  if (warp) ln_backward_kernel<T, VEC, PACKS, true><<<grid, threads, smem, st>>>((const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, a.rows, (int)a.cols, w, a.mean, a.rstd, (T*)a.dx, a.ld_dx, a.ws);
-  else ln_backward_kernel<T, VEC, PACKS, false><<<grid, threads, smem, st>>>((const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, a.rows, (int)a.cols, w, a.mean, a.rstd, (T*)a.dx, a.ld_dx, a.ws);
+template <typename T, int VEC, int PACKS, int CTA>
+cudaError_t backward_cta(const NormBackward& a, Shape s, cudaStream_t st) {
+  constexpr int R = rows_per_step(VEC * PACKS * (int)sizeof(T));
+  const int beside = s.threads / s.width;
+  const size_t smem = std::max<size_t>(Ring<T, VEC, PACKS, 2 * R, kBackwardStages, CTA>::bytes(beside, (int)a.cols), beside > 1 ? (size_t)beside * 2 * a.cols * 4 : 0);
+  static int known[17];
+  const int grid = std::min(back_ctas(a.rows, (int64_t)beside * R), resident((const void*)ln_backward_kernel<T, VEC, PACKS, CTA>, s.threads, smem, known));
+  ln_backward_kernel<T, VEC, PACKS, CTA><<<grid, s.threads, smem, st>>>(s.width, (const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, a.rows, (int)a.cols, Weight{a.weight, a.weight_type}, a.mean, a.rstd,
+                                                                        (T*)a.dx, a.ld_dx, a.ws);
   const cudaError_t e = cudaGetLastError();
   return e != cudaSuccess ? e : backward_join(a, grid, st);
+}
+template <typename T, int VEC, int PACKS>
+cudaError_t backward_form(const NormBackward& a, cudaStream_t st) {
+  const Shape s = shape_of<VEC * PACKS>(a.cols);
+  if constexpr (VEC * PACKS == 16) { if (s.threads > kCtaThreads) return backward_cta<T, VEC, PACKS, kGroupMax>(a, s, st); }
+  return backward_cta<T, VEC, PACKS, kCtaThreads>(a, s, st);
 }
 template <typename T>
 cudaError_t backward_type(const NormBackward& a, cudaStream_t st) {
   if (a.rows == 0) return backward_join(a, 0, st);
+  const int bytes = std::min({pack_bytes(a.x, a.ld_x, a.cols, sizeof(T)), pack_bytes(a.dy, a.ld_dy, a.cols, sizeof(T)), pack_bytes(a.dx, a.ld_dx, a.cols, sizeof(T))});
   if (a.cols > kNormCols) {
-    const Weight w{a.weight, a.weight_type};
     const int split = back_ctas(a.rows, 32);                     // first, since dx may lie where dy or x does
-    ln_columns_kernel<T><<<dim3((unsigned)((a.cols + 255) / 256), split), 256, 0, st>>>((const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, a.rows, (int)a.cols, a.mean, a.rstd, a.ws);
-    ln_backward_long_kernel<T><<<(unsigned)a.rows, kLongThreads, 0, st>>>((const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, (int)a.cols, w, a.mean, a.rstd, (T*)a.dx, a.ld_dx);
+    auto launch = [&](auto columns, auto kernel, int vec) {
+      columns<<<dim3((unsigned)((a.cols + 256 * vec - 1) / (256 * vec)), split), 256, 0, st>>>((const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, a.rows, (int)a.cols, a.mean, a.rstd, a.ws);
+      kernel<<<(unsigned)a.rows, kLongThreads, 0, st>>>((const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, (int)a.cols, Weight{a.weight, a.weight_type}, a.mean, a.rstd, (T*)a.dx, a.ld_dx);
+    };
+    if (bytes == 16) launch(ln_columns_kernel<T, 16 / sizeof(T)>, ln_backward_long_kernel<T, 16 / sizeof(T)>, 16 / (int)sizeof(T));
+    else launch(ln_columns_kernel<T, 1>, ln_backward_long_kernel<T, 1>, 1);
     const cudaError_t e = cudaGetLastError();
     return e != cudaSuccess ? e : backward_join(a, split, st);
   }
-  const int bytes = std::min({pack_bytes(a.x, a.ld_x, a.cols, sizeof(T)), pack_bytes(a.dy, a.ld_dy, a.cols, sizeof(T)), pack_bytes(a.dx, a.ld_dx, a.cols, sizeof(T))});
   return by_form<T>(bytes, a.cols, [&](auto f) { return backward_form<T, decltype(f)::kVec, decltype(f)::kPacks>(a, st); });
 }
 
@@ -572,12 +657,12 @@ int layer_norm_configure() {
   auto each = [&](auto t) {
     using T = decltype(t);
     for (int bytes : {16, 4, (int)sizeof(T)})
-      for (int64_t cols : {1, kGroupMax * 16, kNormCols})
+      for (int64_t cols : {1, kNormCols})
         by_form<T>(bytes, cols, [&](auto f) {
           constexpr int VEC = decltype(f)::kVec, PACKS = decltype(f)::kPacks;
           auto room = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024); };
-          room(ln_forward_kernel<T, VEC, PACKS, true>); room(ln_forward_kernel<T, VEC, PACKS, false>);
-          room(ln_backward_kernel<T, VEC, PACKS, true>); room(ln_backward_kernel<T, VEC, PACKS, false>);
+          room(ln_forward_kernel<T, VEC, PACKS, kCtaThreads>); room(ln_backward_kernel<T, VEC, PACKS, kCtaThreads>);
+          if constexpr (VEC * PACKS == 16) { room(ln_forward_kernel<T, VEC, PACKS, kGroupMax>); room(ln_backward_kernel<T, VEC, PACKS, kGroupMax>); }
           return e;
         });
   };
