@@ -272,8 +272,9 @@ typedef struct { const void* data; /* DEVICE */ int64_t n; int32_t type; /* atom
  * out[0] = sqrt(sum of the squares of all elements of all tensors), out[1] = min(1, max_norm / (out[0] + 1e-6)): the norm and the
  * factor that clips the gradients to it.  max_norm > 0; INFINITY asks for the norm alone (factor 1).  The sum neither
  * overflows nor underflows: out[0] is the norm rounded to fp32.  Where an element is NaN or Inf the norm is not finite and
- * the factor is NaN.  Tensors may be empty; at most 2^20 of them.  workspace: atomo_grad_norm_workspace_bytes().               */
-int64_t atomo_grad_norm_workspace_bytes(void);
+ * the factor is NaN.  Tensors may be empty; at most 2^20 of them.  workspace: atomo_grad_norm_workspace_bytes (0, and NULL will do, where little is
+ * to be read; -1 on bad arguments).                                                                                              */
+int64_t atomo_grad_norm_workspace_bytes(const atomo_tensor* grads /*HOST array*/, int32_t n_tensors);
 int atomo_grad_norm(atomo_ctx* ctx, const atomo_tensor* grads /*HOST array*/, int32_t n_tensors, double max_norm,
                     float* out /*DEVICE, 2 floats*/, void* workspace /*DEVICE*/, int64_t workspace_bytes, void* stream);
 
@@ -331,7 +332,7 @@ int atomo_embedding_backward(atomo_ctx* ctx, const void* ids /*DEVICE*/, int32_t
  * Over the cols values of each row: y = (x - mean) rstd weight + bias, rstd = 1 / sqrt(variance + eps).  x and y are rows x cols of `type` with
  * leading dimensions; weight and bias (either may be NULL: ones, zeros) cols values of weight_type; mean and rstd fp32[rows] are kept for the
  * backward pass, which gives dx (rows x cols of `type`) and, where not NULL, the sums over the rows dweight and dbias (fp32[cols]).
- * y may be x, and dx may be dy or x (same leading dimension).  0 <= rows < 2^31, 1 <= cols <= 2^24, eps >= 0.
+ * y may be x, and dx may be dy or x (same leading dimension).  0 <= rows <= 2^30, 1 <= cols <= 2^24, eps >= 0.
  * workspace: atomo_layer_norm_workspace_bytes (-1 on bad arguments).                                                               */
 int atomo_layer_norm(atomo_ctx* ctx, const void* x /*DEVICE*/, int32_t type, int64_t rows, int64_t cols, int64_t ld, const void* weight /*DEVICE or NULL*/,
                      const void* bias /*DEVICE or NULL*/, int32_t weight_type, double eps, void* y /*DEVICE*/, int64_t ld_y, float* mean /*DEVICE*/,

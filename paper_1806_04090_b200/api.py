@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 from dataclasses import dataclass, field
 from typing import List, Optional, Sequence
 
@@ -148,10 +149,11 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.atomo_measure_fma_peak.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_double)]
     lib.atomo_decode_spectral_static.argtypes = [ctypes.c_int, vp, ctypes.POINTER(i64), ctypes.POINTER(i64),
                                                  ctypes.POINTER(vp), i32, vp]
-    lib.atomo_grad_norm_workspace_bytes.argtypes = []
+    # (descriptors of these are packed bytes: filling ctypes structures takes longer than a kernel launch)
+    lib.atomo_grad_norm_workspace_bytes.argtypes = [vp, i32]
     lib.atomo_grad_norm_workspace_bytes.restype = i64
-    lib.atomo_grad_norm.argtypes = [vp, ctypes.POINTER(_Tensor), i32, dbl, vp, vp, i64, vp]
-    lib.atomo_adamw.argtypes = [vp, ctypes.POINTER(_AdamWTensor), ctypes.POINTER(vp), i32, ctypes.POINTER(_AdamWArgs), vp]
+    lib.atomo_grad_norm.argtypes = [vp, vp, i32, dbl, vp, vp, i64, vp]
+    lib.atomo_adamw.argtypes = [vp, vp, vp, i32, vp, vp]
     lib.atomo_embedding.argtypes = [vp, vp, i32, i64, i64, i64, vp, i32, i64, dbl, vp, i64, vp, vp]
     lib.atomo_embedding_workspace_bytes.argtypes = [i64, i64, i64]
     lib.atomo_embedding_workspace_bytes.restype = i64
@@ -212,9 +214,7 @@ def measure_fma_peak(device: int = 0, fp64: bool = False) -> float:
     return float(out.value)
 
 
-@functools.lru_cache(maxsize=1)
-def _grad_norm_bytes() -> int:
-    return int(load_library().atomo_grad_norm_workspace_bytes())
+_ADAMW_ARGS = struct.Struct("=ddddqQQii").pack          # _AdamWArgs
 
 
 def default_k_cap(s: float, n_atoms: int) -> int:
@@ -643,6 +643,7 @@ class Atomo:
         return [float(x) for x in out]
 
     # ---- operators on either side of the exchange ---------------------------------------------
+    # (Small calls take as long as their host side: what is a C call on a tensor, an allocation or a ctypes object is counted here.)
     def _own_stream(self, stream: Optional[torch.cuda.Stream]) -> int:
         """The stream given, or the current one of the context's device (whatever device is current)."""
         if stream is None:
@@ -668,20 +669,24 @@ class Atomo:
         """Two fp32 numbers on the device: the 2-norm over all elements of all gradients, and min(1, max_norm / (norm + 1e-6)), the factor
         that clips them (NaN where the norm is not finite), as atomo_adamw takes them.  Gradients: contiguous fp32, bf16 or fp16."""
         device, codes = self.device, TYPE_CODES
-        desc = []
+        desc = []                                        # of _Tensor
         for g in grads:
             code = codes.get(g.dtype)
             if code is None or g.get_device() != device or not g.is_contiguous():
                 raise ValueError(f"gradients must be contiguous fp32, bf16 or fp16 tensors on CUDA device {device}")
-            desc.append((g.data_ptr(), g.numel(), code, 0))
-        n = len(desc)
+            desc += (g.data_ptr(), g.numel(), code)
+        n = len(desc) // 3
         if out is None:
             out = torch.empty(2, dtype=torch.float32, device=self._torch_device)
         elif not (out.get_device() == device and out.dtype == torch.float32 and out.numel() == 2 and out.is_contiguous()):
             raise ValueError(f"out: two fp32 numbers on CUDA device {device} are required")
         s = self._own_stream(stream)
-        ws = self._scratch(_grad_norm_bytes(), stream)
-        self._check(self.lib.atomo_grad_norm(self._h, (_Tensor * n)(*desc), n, float(max_norm), out.data_ptr(), ws.data_ptr(), ws.numel(), s), "atomo_grad_norm")
+        packed = struct.pack("=" + "qqq" * n, *desc)     # (the type's high half is the reserved word)
+        nbytes = self.lib.atomo_grad_norm_workspace_bytes(packed, n)
+        if nbytes < 0:
+            raise AtomoError(1, "atomo_grad_norm_workspace_bytes")
+        ws = self._scratch(nbytes, stream) if nbytes else None
+        self._check(self.lib.atomo_grad_norm(self._h, packed, n, max_norm, out.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, s), "atomo_grad_norm")
         return out
 
     def atomo_adamw(self, state: AdamWState, grads: Sequence[torch.Tensor], lr: float, step: int, beta1: float = 0.9, beta2: float = 0.999,
@@ -704,8 +709,8 @@ class Atomo:
             ptrs.append(g.data_ptr())
         if scale is not None and not (scale.get_device() == device and scale.dtype == torch.float32 and scale.numel() == 2 and scale.is_contiguous()):
             raise ValueError(f"scale: two fp32 numbers on CUDA device {device} are required")
-        args = _AdamWArgs(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, None if scale is None else scale.data_ptr(), state.bits, TYPE_CODES[kind])
-        rc = self.lib.atomo_adamw(self._h, state._desc, (ctypes.c_void_p * n)(*ptrs), n, ctypes.byref(args), self._own_stream(stream))
+        args = _ADAMW_ARGS(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, 0 if scale is None else scale.data_ptr(), state.bits, TYPE_CODES[kind])
+        rc = self.lib.atomo_adamw(self._h, state._desc, struct.pack("=%dQ" % n, *ptrs), n, args, self._own_stream(stream))
         self._check(rc, "atomo_adamw")
 
     def _status(self, status: Optional[torch.Tensor]):
@@ -724,22 +729,22 @@ class Atomo:
                         status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """scale * table[ids], of shape ids.shape + (cols,).  An id outside the table gives a row of zeros and raises `status` (one int32, set to
         zero by the caller) to ATOMO_ERR_INVALID_ARG."""
-        code = TYPE_CODES[self._operand(table, "table").dtype]
+        kind = self._operand(table, "table").dtype
         if table.dim() != 2:
             raise ValueError("table: a matrix is required")
-        cols = table.shape[1]
-        rows, ld = _rows(table, cols, "table")
+        rows, cols = table.shape
+        ld = cols if table.is_contiguous() else _rows(table, cols, "table")[1]
         width = self._ids(ids)
         n = ids.numel()
         if out is None:
-            out = torch.empty((*ids.shape, cols), dtype=table.dtype, device=table.device)
+            out = table.new_empty((n, cols)) if ids.dim() == 1 else table.new_empty((*ids.shape, cols))
             ld_out = cols
         else:
-            n_out, ld_out = _rows(self._operand(out, "out", (table.dtype,)), cols, "out")
+            n_out, ld_out = _rows(self._operand(out, "out", (kind,)), cols, "out")
             if n_out != n:
                 raise ValueError(f"out: {n} rows are required")
-        rc = self.lib.atomo_embedding(self._h, table.data_ptr(), code, rows, cols, ld, ids.data_ptr(), width, n, scale, out.data_ptr(), ld_out,
-                                      self._status(status), self._own_stream(stream))
+        rc = self.lib.atomo_embedding(self._h, table.data_ptr(), TYPE_CODES[kind], rows, cols, ld, ids.data_ptr(), width, n, scale, out.data_ptr(), ld_out,
+                                      self._status(status) if status is not None else None, self._own_stream(stream))
         self._check(rc, "atomo_embedding")
         return out
 
@@ -753,18 +758,18 @@ class Atomo:
         if grad.dim() < 1 or grad.shape[:-1] != ids.shape:
             raise ValueError("grad: the shape of ids with one more dimension is required")
         n, cols = ids.numel(), grad.shape[-1]
-        _, ld = _rows(grad, cols, "grad") if n and cols else (0, max(cols, 1))
+        ld = cols if grad.is_contiguous() else _rows(grad, cols, "grad")[1] if n and cols else max(cols, 1)
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs out")
-            out = torch.empty((rows, cols), dtype=torch.float32, device=grad.device)
+            out = torch.empty(rows, cols, dtype=torch.float32, device=self._torch_device)
             ld_out = cols
         else:
             n_out, ld_out = _rows(self._operand(out, "out", (torch.float32,)), cols, "out")
             if n_out != rows:
                 raise ValueError(f"out: {rows} rows are required")
         s = self._own_stream(stream)
-        nbytes = int(self.lib.atomo_embedding_workspace_bytes(n, rows, cols))
+        nbytes = self.lib.atomo_embedding_workspace_bytes(n, rows, cols)
         if nbytes < 0:
             raise AtomoError(1, "atomo_embedding_workspace_bytes")
         ws = self._scratch(nbytes, stream)
@@ -773,35 +778,38 @@ class Atomo:
         self._check(rc, "atomo_embedding_backward")
         return out
 
-    def _weight(self, weight, bias, cols: int):
-        """(pointers of weight and bias, type code) of a layer norm's parameters, either of which may be None."""
-        kinds = {t.dtype for t in (weight, bias) if t is not None}
-        if len(kinds) > 1:
-            raise ValueError("weight and bias must have one type")
-        for name, t in (("weight", weight), ("bias", bias)):
-            if t is not None and not (self._operand(t, name).is_contiguous() and t.numel() == cols):
-                raise ValueError(f"{name}: a contiguous tensor of {cols} elements is required")
-        ptr = lambda t: None if t is None else t.data_ptr()
-        return ptr(weight), ptr(bias), TYPE_CODES[kinds.pop()] if kinds else 0
+    def _weight(self, weight, cols: int, what: str):
+        """(pointer, type) of a layer norm's weight or bias, which may be None."""
+        if weight is None:
+            return None, None
+        kind = self._operand(weight, what).dtype
+        if weight.numel() != cols or not weight.is_contiguous():
+            raise ValueError(f"{what}: a contiguous tensor of {cols} elements is required")
+        return weight.data_ptr(), kind
 
     def atomo_layer_norm(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
                          out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
         """Layer norm over the last dimension: (y, mean, rstd), y of x's type and shape, mean and rstd in fp32 with one value per row.  out may
         be x."""
-        code = TYPE_CODES[self._operand(x, "x").dtype]
-        cols = x.shape[-1] if x.dim() else 0
-        rows, ld = _rows(x, cols, "x") if x.numel() else (0, max(cols, 1))
-        w, b, wcode = self._weight(weight, bias, cols)
+        kind = self._operand(x, "x").dtype
+        shape = x.shape
+        cols = shape[-1] if shape else 0
+        w, wkind = self._weight(weight, cols, "weight")
+        b, bkind = self._weight(bias, cols, "bias")
+        if w is not None and b is not None and wkind is not bkind:
+            raise ValueError("weight and bias must have one type")
+        rows, ld = (x.numel() // max(cols, 1), cols) if x.is_contiguous() else _rows(x, cols, "x")
         if out is None:
-            out, ld_out = torch.empty(x.shape, dtype=x.dtype, device=x.device), cols
+            out, ld_out = (torch.empty_like(x) if ld == cols else torch.empty(shape, dtype=kind, device=x.device)), cols
         else:
-            if self._operand(out, "out", (x.dtype,)).shape != x.shape:
+            if self._operand(out, "out", (kind,)).shape != shape:
                 raise ValueError("out: the shape of x is required")
-            _, ld_out = _rows(out, cols, "out") if x.numel() else (0, max(cols, 1))
-        stats = torch.empty((2, *x.shape[:-1]), dtype=torch.float32, device=x.device)
-        mean, rstd = stats.unbind(0)
-        rc = self.lib.atomo_layer_norm(self._h, x.data_ptr(), code, rows, cols, ld, w, b, wcode, eps, out.data_ptr(), ld_out, mean.data_ptr(), rstd.data_ptr(),
-                                       self._own_stream(stream))
+            ld_out = cols if out.is_contiguous() else _rows(out, cols, "out")[1]
+        lines = rows if len(shape) == 2 else shape[:-1]
+        mean = torch.empty(lines, dtype=torch.float32, device=self._torch_device)
+        rstd = torch.empty(lines, dtype=torch.float32, device=self._torch_device)
+        rc = self.lib.atomo_layer_norm(self._h, x.data_ptr(), TYPE_CODES[kind], rows, cols, ld, w, b, TYPE_CODES[wkind or bkind or kind], eps, out.data_ptr(), ld_out,
+                                       mean.data_ptr(), rstd.data_ptr(), self._own_stream(stream))
         self._check(rc, "atomo_layer_norm")
         return out, mean, rstd
 
@@ -809,30 +817,32 @@ class Atomo:
                                   out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
         """(dx, dweight, dbias) of atomo_layer_norm: dx of x's type, dweight and dbias in fp32, whatever the weight's type.  out (for dx) may
         be dy or x."""
-        code = TYPE_CODES[self._operand(x, "x").dtype]
-        self._operand(dy, "dy", (x.dtype,))
-        cols = x.shape[-1] if x.dim() else 0
-        if dy.shape != x.shape:
+        kind = self._operand(x, "x").dtype
+        self._operand(dy, "dy", (kind,))
+        shape = x.shape
+        cols = shape[-1] if shape else 0
+        if dy.shape != shape:
             raise ValueError("dy: the shape of x is required")
-        rows, ld = _rows(x, cols, "x") if x.numel() else (0, max(cols, 1))
-        _, ld_dy = _rows(dy, cols, "dy") if x.numel() else (0, max(cols, 1))
+        rows, ld = (x.numel() // max(cols, 1), cols) if x.is_contiguous() else _rows(x, cols, "x")
+        ld_dy = cols if dy.is_contiguous() else _rows(dy, cols, "dy")[1]
         for name, t in (("mean", mean), ("rstd", rstd)):
-            if not (self._operand(t, name, (torch.float32,)).is_contiguous() and t.numel() == rows):
-                raise ValueError(f"{name}: {rows} contiguous fp32 numbers are required")
-        w, _, wcode = self._weight(weight, None, cols)
+            if t.dtype != torch.float32 or t.get_device() != self.device or t.numel() != rows or not t.is_contiguous():
+                raise ValueError(f"{name}: {rows} contiguous fp32 numbers on CUDA device {self.device} are required")
+        w, wkind = self._weight(weight, cols, "weight")
         if out is None:
-            out, ld_dx = torch.empty(x.shape, dtype=x.dtype, device=x.device), max(cols, 1)
+            out, ld_dx = (torch.empty_like(x) if ld == cols else torch.empty(shape, dtype=kind, device=x.device)), cols
         else:
-            if self._operand(out, "out", (x.dtype,)).shape != x.shape:
+            if self._operand(out, "out", (kind,)).shape != shape:
                 raise ValueError("out: the shape of x is required")
-            _, ld_dx = _rows(out, cols, "out") if x.numel() else (0, max(cols, 1))
-        dweight, dbias = torch.empty((2, cols), dtype=torch.float32, device=x.device).unbind(0)
+            ld_dx = cols if out.is_contiguous() else _rows(out, cols, "out")[1]
+        dweight = torch.empty(cols, dtype=torch.float32, device=self._torch_device)
+        dbias = torch.empty(cols, dtype=torch.float32, device=self._torch_device)
         s = self._own_stream(stream)
-        nbytes = int(self.lib.atomo_layer_norm_workspace_bytes(rows, cols))
+        nbytes = self.lib.atomo_layer_norm_workspace_bytes(rows, cols)
         if nbytes < 0:
             raise AtomoError(1, "atomo_layer_norm_workspace_bytes")
         ws = self._scratch(nbytes, stream)
-        rc = self.lib.atomo_layer_norm_backward(self._h, dy.data_ptr(), ld_dy, x.data_ptr(), ld, code, rows, cols, w, wcode, mean.data_ptr(), rstd.data_ptr(),
+        rc = self.lib.atomo_layer_norm_backward(self._h, dy.data_ptr(), ld_dy, x.data_ptr(), ld, TYPE_CODES[kind], rows, cols, w, TYPE_CODES[wkind or kind], mean.data_ptr(), rstd.data_ptr(),
                                                 out.data_ptr(), ld_dx, dweight.data_ptr(), dbias.data_ptr(), ws.data_ptr(), nbytes, s)
         self._check(rc, "atomo_layer_norm_backward")
         return out, dweight, dbias

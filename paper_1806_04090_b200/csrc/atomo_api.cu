@@ -370,9 +370,14 @@ bool bad_type(int type) { return type < ATOMO_TYPE_F32 || type > ATOMO_TYPE_F16;
 bool off_type(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
 // null, or not aligned to its elements
 bool bad_ptr(const void* p, int bytes) { return !p || off_type(p, bytes); }
-constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1, kMostCols = (int64_t)1 << 24;
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1, kMostCols = (int64_t)1 << 24, kNormRows = (int64_t)1 << 30;
 // rows x cols with a leading dimension: offsets stay within 62 bits
 bool bad_shape(int64_t rows, int64_t cols, int64_t ld) { return rows < 0 || rows > kMostRows || cols <= 0 || cols > kMostCols || ld < cols || ld > (int64_t)1 << 31; }
+bool bad_tensors(const atomo_tensor* t, int32_t n) {
+  if (!t || n <= 0 || n > 1 << 20) return true;
+  for (int i = 0; i < n; ++i) if (t[i].n < 0 || t[i].n > (int64_t)1 << 40 || bad_type(t[i].type)) return true;
+  return false;
+}
 // runs f on the context's device; nothing is thrown through the C boundary
 template <typename F> int on_device(atomo_ctx* ctx, const char* what, F f) {
   try {
@@ -1504,16 +1509,17 @@ int atomo_decode_average(atomo_ctx* ctx, int32_t kind, const void* const* payloa
 // ==================================================================================================
 // Operators on either side of the exchange.  They use nothing of the context but its device and its error text.
 
-int64_t atomo_grad_norm_workspace_bytes(void) { return (int64_t)kNormSlots * sizeof(double); }
+int64_t atomo_grad_norm_workspace_bytes(const atomo_tensor* grads, int32_t n_tensors) {
+  if (bad_tensors(grads, n_tensors)) return -1;
+  return grad_norm_slots(grads, n_tensors) * (int64_t)sizeof(double);
+}
 
 int atomo_grad_norm(atomo_ctx* ctx, const atomo_tensor* grads, int32_t n_tensors, double max_norm, float* out, void* workspace, int64_t workspace_bytes, void* stream) {
-  if (!ctx || !grads || n_tensors <= 0 || n_tensors > 1 << 20 || !(max_norm > 0.0) || bad_ptr(out, 4)) return ATOMO_ERR_INVALID_ARG;
-  for (int i = 0; i < n_tensors; ++i) {
-    const atomo_tensor& t = grads[i];
-    if (t.n < 0 || t.n > (int64_t)1 << 40 || bad_type(t.type) || (t.n > 0 && bad_ptr(t.data, type_bytes(t.type)))) return ATOMO_ERR_INVALID_ARG;
-  }
-  if (bad_ptr(workspace, 8)) return ATOMO_ERR_INVALID_ARG;
-  if (workspace_bytes < atomo_grad_norm_workspace_bytes()) return ATOMO_ERR_CAPACITY;
+  if (!ctx || bad_tensors(grads, n_tensors) || !(max_norm > 0.0) || bad_ptr(out, 4)) return ATOMO_ERR_INVALID_ARG;
+  for (int i = 0; i < n_tensors; ++i) if (grads[i].n > 0 && bad_ptr(grads[i].data, type_bytes(grads[i].type))) return ATOMO_ERR_INVALID_ARG;
+  const int64_t need = atomo_grad_norm_workspace_bytes(grads, n_tensors);
+  if (need > 0 && bad_ptr(workspace, 8)) return ATOMO_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return ATOMO_ERR_CAPACITY;
   return on_device(ctx, "gradient norm", [&] { return launch_grad_norm(grads, n_tensors, max_norm, out, static_cast<double*>(workspace), (cudaStream_t)stream); });
 }
 
@@ -1569,7 +1575,7 @@ int atomo_embedding_backward(atomo_ctx* ctx, const void* ids, int32_t id_bytes, 
 
 int atomo_layer_norm(atomo_ctx* ctx, const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ld, const void* weight, const void* bias, int32_t weight_type,
                      double eps, void* y, int64_t ld_y, float* mean, float* rstd, void* stream) {
-  if (!ctx || bad_type(type) || bad_type(weight_type) || bad_shape(rows, cols, ld) || bad_shape(rows, cols, ld_y) || !(eps >= 0.0) || !std::isfinite(eps)) return ATOMO_ERR_INVALID_ARG;
+  if (!ctx || bad_type(type) || bad_type(weight_type) || rows > kNormRows || bad_shape(rows, cols, ld) || bad_shape(rows, cols, ld_y) || !(eps >= 0.0) || !std::isfinite(eps)) return ATOMO_ERR_INVALID_ARG;
   if (off_type(weight, type_bytes(weight_type)) || off_type(bias, type_bytes(weight_type))) return ATOMO_ERR_INVALID_ARG;
   if (rows > 0 && (bad_ptr(x, type_bytes(type)) || bad_ptr(y, type_bytes(type)) || bad_ptr(mean, 4) || bad_ptr(rstd, 4))) return ATOMO_ERR_INVALID_ARG;
   const NormForward a{x, type, rows, cols, ld, weight, bias, weight_type, (float)eps, y, ld_y, mean, rstd};
@@ -1577,14 +1583,14 @@ int atomo_layer_norm(atomo_ctx* ctx, const void* x, int32_t type, int64_t rows, 
 }
 
 int64_t atomo_layer_norm_workspace_bytes(int64_t rows, int64_t cols) {
-  if (bad_shape(rows, cols, cols)) return -1;
+  if (rows > kNormRows || bad_shape(rows, cols, cols)) return -1;
   return (int64_t)layer_norm_workspace(rows, cols);
 }
 
 int atomo_layer_norm_backward(atomo_ctx* ctx, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x, int32_t type, int64_t rows, int64_t cols, const void* weight,
                               int32_t weight_type, const float* mean, const float* rstd, void* dx, int64_t ld_dx, float* dweight, float* dbias,
                               void* workspace, int64_t workspace_bytes, void* stream) {
-  if (!ctx || bad_type(type) || bad_type(weight_type) || bad_shape(rows, cols, ld_dy) || bad_shape(rows, cols, ld_x) || bad_shape(rows, cols, ld_dx)) return ATOMO_ERR_INVALID_ARG;
+  if (!ctx || bad_type(type) || bad_type(weight_type) || rows > kNormRows || bad_shape(rows, cols, ld_dy) || bad_shape(rows, cols, ld_x) || bad_shape(rows, cols, ld_dx)) return ATOMO_ERR_INVALID_ARG;
   if (off_type(weight, type_bytes(weight_type)) || off_type(dweight, 4) || off_type(dbias, 4)) return ATOMO_ERR_INVALID_ARG;
   const int size = type_bytes(type);
   if (rows > 0 && (bad_ptr(dy, size) || bad_ptr(x, size) || bad_ptr(dx, size) || bad_ptr(mean, 4) || bad_ptr(rstd, 4) || bad_ptr(workspace, 16))) return ATOMO_ERR_INVALID_ARG;

@@ -69,8 +69,8 @@ cudaError_t launch_after(void (*kernel)(P...), dim3 grid, dim3 block, size_t sme
 }
 
 // ---- gradient norm (atomo_step.cu) ----------------------------------------------------------------
-// most partial sums of a call, 8 bytes each
-constexpr int kNormSlots = 148 * 8;
+constexpr int kNormSlots = 148 * 8;     // partial sums of a call, at most
+int grad_norm_slots(const atomo_tensor* grads, int n);                           // how many a call needs: 0 where one cluster does it all
 int launch_grad_norm(const atomo_tensor* grads, int n, double max_norm, float* out, double* slots, cudaStream_t st);   // cudaError_t
 
 // ---- AdamW (atomo_step.cu) ------------------------------------------------------------------------

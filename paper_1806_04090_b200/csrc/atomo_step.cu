@@ -183,16 +183,29 @@ __global__ void norm_empty_kernel(double max_norm, float* out) { norm_finish(0.0
 
 }  // namespace
 
+namespace {
+constexpr int kNormMost = 1024;                                  // tensors of a launch, 24 bytes each: 24 KB of kernel arguments
+struct NormPlan { int tensors = 0; uint64_t chunks = 0; bool one = false; };   // one: few enough chunks for one cluster
+NormPlan norm_plan(const atomo_tensor* grads, int n) {
+  NormPlan p;
+  for (int i = 0; i < n; ++i) if (grads[i].n > 0) { ++p.tensors; p.chunks += norm_chunks(grads[i]); }
+  p.one = p.tensors <= kNormMost && p.chunks <= 8 * kNormCluster;
+  return p;
+}
+}  // namespace
+
+int grad_norm_slots(const atomo_tensor* grads, int n) { return norm_plan(grads, n).one ? 0 : kNormSlots; }
+
 int launch_grad_norm(const atomo_tensor* grads, int n, double max_norm, float* out, double* slots, cudaStream_t st) {
-  constexpr int kMost = 1024;                                    // 24 bytes each: 24 KB of kernel arguments
-  std::vector<int> index;
-  uint64_t chunks = 0;
-  for (int i = 0; i < n; ++i) if (grads[i].n > 0) { index.push_back(i); chunks += norm_chunks(grads[i]); }
-  const int m = (int)index.size();
+  constexpr int kMost = kNormMost;
+  const NormPlan plan = norm_plan(grads, n);
+  const int m = plan.tensors;
   if (m == 0) { norm_empty_kernel<<<1, 1, 0, st>>>(max_norm, out); return (int)cudaGetLastError(); }
-  // A few chunks: one cluster does it all.
-  if (m <= kMost && chunks <= 8 * kNormCluster) {
-    const int grid = (int)std::min<uint64_t>(chunks, kNormCluster);
+  std::vector<int> index;
+  index.reserve(m);
+  for (int i = 0; i < n; ++i) if (grads[i].n > 0) index.push_back(i);
+  if (plan.one) {
+    const int grid = (int)std::min<uint64_t>(plan.chunks, kNormCluster);
     if (m <= 8) return (int)norm_batch<8>(grads, index.data(), m, grid, true, 0, max_norm, out, slots, st);
     if (m <= 128) return (int)norm_batch<128>(grads, index.data(), m, grid, true, 0, max_norm, out, slots, st);
     return (int)norm_batch<kMost>(grads, index.data(), m, grid, true, 0, max_norm, out, slots, st);

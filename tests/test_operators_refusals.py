@@ -24,9 +24,13 @@ def ctx():
 
 def test_grad_norm(ctx):
     lib, h = ctx
-    need = lib.atomo_grad_norm_workspace_bytes()
+    size = lib.atomo_grad_norm_workspace_bytes
+    one = lambda n, kind=0: (api._Tensor * 1)((GOOD, n, kind, 0))
+    assert size(one(4), 1) == 0 and size(one(1 << 30), 1) > 0 and size(one(0), 1) >= 0
+    assert size(one(-1), 1) == size(one(4, 3), 1) == size(one(4), 0) == size(None, 1) == -1
+    need = size(one(1 << 24), 1)
 
-    def call(data=GOOD, n=4, kind=0, count=1, max_norm=1.0, out=GOOD, ws=GOOD, size=need):
+    def call(data=GOOD, n=1 << 24, kind=0, count=1, max_norm=1.0, out=GOOD, ws=GOOD, size=need):
         return lib.atomo_grad_norm(h, (api._Tensor * 1)((data, n, kind, 0)), count, max_norm, out, ws, size, None)
 
     for bad in (dict(data=None), dict(data=GOOD + 2), dict(data=GOOD + 1, kind=1), dict(n=-1), dict(kind=3), dict(kind=-1), dict(count=0), dict(count=-1), dict(count=2 ** 20 + 1),
