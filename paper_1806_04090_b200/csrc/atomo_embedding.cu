@@ -12,6 +12,9 @@
 //                     starts in, or in the next one, is summed by the former and goes to its row; a longer one leaves one part per chunk in the workspace.
 //   emb_join_kernel   adds the parts of the longer runs, in order.
 // What bounds it is memory: dout is read once, the table's gradient written once.
+// Short lists go through emb_direct_kernel, which does all of it: a CTA has every so-manieth row of the table (frequent ids often lie side by side) and some
+// columns, finds the tokens of its rows among all ids, sorts them in shared memory and sums them; and it has a stretch of rows in which it writes those without
+// tokens.  A launch instead of three, and no wait between them.
 #include <algorithm>
 
 #include "atomo_ops.cuh"
@@ -123,6 +126,15 @@ __device__ __forceinline__ uint64_t sort_item(const SortArgs& a, int64_t t) {
 // a run is long if it goes on behind the chunk that follows the one it starts in
 __device__ __forceinline__ uint32_t item_id(const uint64_t* items, int64_t i) { return (uint32_t)(items[i] >> 32); }
 
+// a row, by a warp
+__device__ __forceinline__ void zero_row(float* p, int64_t cols, int vec) {
+  int64_t c = threadIdx.x & 31;
+  if (vec) {
+    for (; c < cols / 4; c += 32) reinterpret_cast<float4*>(p)[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    c = cols / 4 * 4 + (threadIdx.x & 31);
+  }
+  for (; c < cols; c += 32) p[c] = 0.0f;
+}
 // rows without tokens, by the CTAs behind those that sort: a range of rows each
 __device__ __forceinline__ void zero_rows(const SortArgs& a, uint8_t* s_seen) {
   constexpr int64_t kFlags = 65536;
@@ -140,13 +152,7 @@ __device__ __forceinline__ void zero_rows(const SortArgs& a, uint8_t* s_seen) {
     __syncthreads();
     for (int64_t r = threadIdx.x >> 5; r < count; r += kSortWarps) {
       if (s_seen[r]) continue;
-      float* p = a.out + (r0 + r) * a.ld_out;
-      int64_t c = threadIdx.x & 31;
-      if (a.vec_out) {
-        for (; c < a.cols / 4; c += 32) reinterpret_cast<float4*>(p)[c] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        c = a.cols / 4 * 4 + (threadIdx.x & 31);
-      }
-      for (; c < a.cols; c += 32) p[c] = 0.0f;
+      zero_row(a.out + (r0 + r) * a.ld_out, a.cols, a.vec_out);
     }
     __syncthreads();
   }
@@ -461,6 +467,142 @@ __global__ void __launch_bounds__(32 * kJoinSlices) emb_join_kernel(const __grid
   }
 }
 
+// ---- short lists, in one launch -------------------------------------------------------------------
+constexpr int kDirectThreads = 512, kDirectWarps = kDirectThreads / 32, kDirectBits = 12, kDirectMost = 1 << kDirectBits;   // tokens at most
+constexpr int kDirectRows = 8192;                                // rows of a CTA's stretch, at most
+struct DirectArgs {
+  Ids ids; int n, padded; int64_t rows, cols, padding;           // padded: a power of two that holds n
+  const void* dout; int64_t ld;
+  float scale; int accumulate;
+  float* out; int64_t ld_out; int vec_out;
+  int32_t* status; int per;                                      // rows of a CTA's stretch
+};
+template <typename T, int VEC> struct DirectShape {              // columns of a CTA: 32 lanes, at least four columns each
+  static constexpr int kPacks = VEC >= 4 ? 1 : 4 / VEC, kCols = 32 * VEC * kPacks;
+};
+
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kDirectThreads, 2) emb_direct_kernel(const __grid_constant__ DirectArgs a) {
+  constexpr int PACKS = DirectShape<T, VEC>::kPacks, COLS = DirectShape<T, VEC>::kCols, kAhead = VEC * sizeof(T) == 16 && sizeof(T) == 2 ? 4 : 8;
+  extern __shared__ uint32_t s_keys[];                           // [padded] row << 13 | token; then [2][warps][COLS] parts of runs, a flag per row
+  float* s_part = reinterpret_cast<float*>(s_keys + a.padded);
+  uint8_t* s_seen = reinterpret_cast<uint8_t*>(s_part + 2 * kDirectWarps * COLS);
+  __shared__ int s_count, s_row[2][kDirectWarps + 1];            // rows of the parts, -1: none
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int64_t c0 = (int64_t)blockIdx.y * COLS;
+  const uint32_t hop = gridDim.x;                                // between two rows of this CTA, the first of which is blockIdx.x
+  const int64_t z0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * a.per;
+  const int rows = a.accumulate ? 0 : (int)max((int64_t)0, min((int64_t)a.per, a.rows - z0));     // of its stretch
+  auto row_at = [&](int i) { return a.out + ((int64_t)i * hop + blockIdx.x) * a.ld_out + c0; };
+  for (int i = tid; i < (rows + 3) / 4; i += kDirectThreads) reinterpret_cast<uint32_t*>(s_seen)[i] = 0u;
+  if (tid == 0) s_count = 0;
+  if (tid <= kDirectWarps) s_row[0][tid] = s_row[1][tid] = -1;
+  __syncthreads();
+  // the tokens of these rows, in any order
+  for (int t0 = warp * 32; t0 < a.n; t0 += kDirectThreads) {
+    const int t = t0 + lane;
+    const int64_t id = t < a.n ? load_id(a.ids, t) : -1;
+    const bool valid = id >= 0 && id < a.rows;
+    if (t < a.n && !valid && blockIdx.x == 0 && blockIdx.y == 0) raise_word(a.status);
+    const uint32_t row = (uint32_t)id / hop;
+    const bool mine = valid && (uint32_t)id - row * hop == blockIdx.x && id != a.padding;
+    const uint32_t ballot = __ballot_sync(0xffffffffu, mine);
+    int at = 0;
+    if (ballot != 0u && lane == 0) at = atomicAdd(&s_count, __popc(ballot));
+    at = __shfl_sync(0xffffffffu, at, 0);
+    if (mine) s_keys[at + __popc(ballot & ((1u << lane) - 1u))] = row << kDirectBits | (uint32_t)t;
+    if (valid && id >= z0 && id < z0 + rows && id != a.padding) s_seen[id - z0] = 1;
+  }
+  __syncthreads();
+  // all keys differ, so that any way to sort them gives the same order: rows, and in a row the tokens, ascending
+  const int count = s_count;
+  int size = 32;
+  while (size < count) size <<= 1;
+  for (int i = count + tid; i < size && i < a.padded; i += kDirectThreads) s_keys[i] = 0xffffffffu;
+  __syncthreads();
+  if (count > 1) {
+    for (int k = 2; k <= size; k <<= 1) {
+      for (int j = k >> 1; j > 0; j >>= 1) {
+        for (int p = tid; p < size / 2; p += kDirectThreads) {
+          const int i = 2 * p - (p & (j - 1)), l = i + j;
+          const uint32_t x = s_keys[i], y = s_keys[l];
+          if ((x > y) == ((i & k) == 0)) { s_keys[i] = y; s_keys[l] = x; }
+        }
+        __syncthreads();
+      }
+    }
+  }
+  // a warp sums a stretch of the sorted tokens; runs that go over its ends leave parts
+  const T* dout = static_cast<const T*>(a.dout) + c0;
+  auto inside = [&](int p) { return c0 + (p * 32 + lane) * VEC < a.cols; };
+  float acc[PACKS][VEC];
+  auto clear = [&] {
+#pragma unroll
+    for (int p = 0; p < PACKS; ++p) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) acc[p][j] = 0.0f;
+    }
+  };
+  const SumArgs put{nullptr, nullptr, 0, 0, a.rows, a.cols, nullptr, 0, a.scale, a.accumulate, a.out, a.ld_out, nullptr, 0, a.vec_out};
+  const int stretch = (count + kDirectWarps - 1) / kDirectWarps, begin = min(warp * stretch, count), end = min(begin + stretch, count);
+  if (begin < end) {
+    int run = (int)(s_keys[begin] >> kDirectBits);
+    bool part = begin > 0 && (int)(s_keys[begin - 1] >> kDirectBits) == run;
+    auto flush = [&](int slot) {
+      if (slot >= 0) {
+        if (lane == 0) s_row[slot][warp] = run;
+#pragma unroll
+        for (int p = 0; p < PACKS; ++p) {
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) s_part[(slot * kDirectWarps + warp) * COLS + (p * 32 + lane) * VEC + j] = acc[p][j];
+        }
+      } else {
+#pragma unroll
+        for (int p = 0; p < PACKS; ++p) if (inside(p)) put_row<VEC>(put, row_at(run) + (p * 32 + lane) * VEC, acc[p]);
+      }
+    };
+    clear();
+    for (int i0 = begin; i0 < end; i0 += kAhead) {
+      Pack<T, VEC> x[kAhead][PACKS];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int64_t token = i0 + u < end ? (int64_t)(s_keys[i0 + u] & (kDirectMost - 1)) : 0;
+#pragma unroll
+        for (int p = 0; p < PACKS; ++p) if (i0 + u < end && inside(p)) x[u][p] = load_pack<T, VEC>(dout + token * a.ld + (p * 32 + lane) * VEC);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (i0 + u < end) {
+          const int row = (int)(s_keys[i0 + u] >> kDirectBits);
+          if (row != run) { flush(part ? 0 : -1); run = row; part = false; clear(); }
+#pragma unroll
+          for (int p = 0; p < PACKS; ++p) {
+            if (inside(p)) {
+#pragma unroll
+              for (int j = 0; j < VEC; ++j) acc[p][j] += to_float(x[u][p].v[j]);
+            }
+          }
+        }
+      }
+    }
+    flush(part ? 0 : end < count && (int)(s_keys[end] >> kDirectBits) == run ? 1 : -1);
+  }
+  for (int r = warp; r < rows; r += kDirectWarps) if (!s_seen[r]) zero_row(a.out + (z0 + r) * a.ld_out, a.cols, a.vec_out);
+  // the runs that went over: their parts in order, a thread per column
+  __syncthreads();
+  if (tid < COLS && c0 + tid < a.cols) {
+    float sum[1] = {0.0f};
+    for (int w = 0; w < kDirectWarps; ++w) {
+      const int over = s_row[0][w];
+      if (over >= 0) {
+        sum[0] += s_part[w * COLS + tid];
+        if (s_row[0][w + 1] != over) put_row<1>(put, row_at(over) + tid, sum);
+      }
+      if (s_row[1][w] >= 0) sum[0] = s_part[(kDirectWarps + w) * COLS + tid];
+    }
+  }
+}
+
 // columns that a thread moves in one piece: 16 bytes where base, leading dimension and length allow it, for 16-bit types also 4 bytes
 int emb_vec(const void* base, int64_t ld, int64_t cols, int size) {
   const uintptr_t p = reinterpret_cast<uintptr_t>(base);
@@ -534,6 +676,30 @@ cudaError_t sum_type(SumArgs& a, cudaStream_t st) {
 
 }  // namespace
 
+namespace {
+template <typename T, int VEC>
+cudaError_t direct_typed(DirectArgs& a, cudaStream_t st) {
+  constexpr int COLS = DirectShape<T, VEC>::kCols;
+  const int slabs = (int)((a.cols + COLS - 1) / COLS);
+  // two CTAs per SM; more where their stretches would get too long, or their rows' numbers not fit the keys
+  int64_t ctas = std::max<int64_t>(1, std::min<int64_t>(a.rows, 2 * 148 / slabs));
+  ctas = std::max({ctas, (a.rows + (int64_t)slabs * kDirectRows - 1) / ((int64_t)slabs * kDirectRows), (a.rows >> (32 - kDirectBits)) + 1});
+  a.per = (int)((a.rows + ctas * slabs - 1) / (ctas * slabs));
+  a.padded = 32;
+  while (a.padded < a.n) a.padded <<= 1;
+  const size_t smem = (size_t)a.padded * 4 + (size_t)2 * kDirectWarps * COLS * 4 + (a.per + 3) / 4 * 4;
+  emb_direct_kernel<T, VEC><<<dim3((unsigned)ctas, slabs), kDirectThreads, smem, st>>>(a);
+  return cudaGetLastError();
+}
+template <typename T>
+cudaError_t direct_type(DirectArgs& a, cudaStream_t st) {
+  const int vec = emb_vec(a.dout, a.ld, a.cols, sizeof(T));
+  if (vec == 16 / (int)sizeof(T)) return direct_typed<T, 16 / sizeof(T)>(a, st);
+  if constexpr (sizeof(T) == 2) { if (vec == 2) return direct_typed<T, 2>(a, st); }
+  return direct_typed<T, 1>(a, st);
+}
+}  // namespace
+
 int embedding_configure(int device) {
   cudaError_t e = cudaFuncSetAttribute(emb_sort_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortTile * 16);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(emb_sort_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortTile * 8);
@@ -542,6 +708,11 @@ int embedding_configure(int device) {
   sum(emb_sum_kernel<float, 4>); sum(emb_sum_kernel<float, 1>);
   sum(emb_sum_kernel<__nv_bfloat16, 8>); sum(emb_sum_kernel<__nv_bfloat16, 2>); sum(emb_sum_kernel<__nv_bfloat16, 1>);
   sum(emb_sum_kernel<__half, 8>); sum(emb_sum_kernel<__half, 2>); sum(emb_sum_kernel<__half, 1>);
+  // 16 KB of keys, 32 KB of parts and 8 KB of flags
+  auto direct = [&](auto kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 57 * 1024); };
+  direct(emb_direct_kernel<float, 4>); direct(emb_direct_kernel<float, 1>);
+  direct(emb_direct_kernel<__nv_bfloat16, 8>); direct(emb_direct_kernel<__nv_bfloat16, 2>); direct(emb_direct_kernel<__nv_bfloat16, 1>);
+  direct(emb_direct_kernel<__half, 8>); direct(emb_direct_kernel<__half, 2>); direct(emb_direct_kernel<__half, 1>);
   if (e != cudaSuccess) return (int)e;
   const bool wide = cudaFuncSetAttribute(emb_sort_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
                     cudaFuncSetAttribute(emb_sort_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
@@ -568,6 +739,15 @@ int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
   if (b.n == 0 && b.accumulate) return (int)cudaSuccess;
   const EmbLayout l = emb_layout(b.n, b.cols);
   const int vec_out = reinterpret_cast<uintptr_t>(b.out) % 16 == 0 && b.ld_out % 4 == 0;
+  // One launch for up to 2048 tokens, and up to 4096 where the gradient is small.  Kernels alone, us, one launch | three (tokens x rows x columns, fp32):
+  // 1 x 50000 x 64 7 | 13, 256 x 21294 x 38 7 | 18, 1000 x 5000 x 64 8 | 22, 1000 x 32000 x 1024 29 | 32, 4001 x 10007 x 515 23 | 24, 4000 x 10000 x 512
+  // 22 | 22, 4000 x 32000 x 2048 69 | 60
+  if (b.n <= 2048 || (b.n <= kDirectMost && b.rows * b.cols <= (int64_t)1 << 23)) {
+    DirectArgs d{};
+    d.ids = Ids{b.ids, b.id_bytes == 8}; d.n = (int)b.n; d.rows = b.rows; d.cols = b.cols; d.padding = b.padding; d.dout = b.grad; d.ld = b.ld;
+    d.scale = b.scale; d.accumulate = b.accumulate; d.out = b.out; d.ld_out = b.ld_out; d.vec_out = vec_out; d.status = b.status;
+    return (int)(b.type == ATOMO_TYPE_F32 ? direct_type<float>(d, st) : b.type == ATOMO_TYPE_BF16 ? direct_type<__nv_bfloat16>(d, st) : direct_type<__half>(d, st));
+  }
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return (int)e;
