@@ -499,28 +499,51 @@ __global__ void __launch_bounds__(kDirectThreads, 2) emb_direct_kernel(const __g
   if (tid <= kDirectWarps) s_row[0][tid] = s_row[1][tid] = -1;
   __syncthreads();
   // the tokens of these rows, in any order
-  for (int t0 = warp * 32; t0 < a.n; t0 += kDirectThreads) {
-    const int t = t0 + lane;
-    const int64_t id = t < a.n ? load_id(a.ids, t) : -1;
-    const bool valid = id >= 0 && id < a.rows;
+  int64_t id[kDirectMost / kDirectThreads];
+#pragma unroll
+  for (int i = 0; i < kDirectMost / kDirectThreads; ++i) { const int t = i * kDirectThreads + tid; id[i] = t < a.n ? load_id(a.ids, t) : -1; }
+#pragma unroll
+  for (int i = 0; i < kDirectMost / kDirectThreads; ++i) {
+    const int t = i * kDirectThreads + tid;
+    if (i * kDirectThreads >= a.n) break;
+    const bool valid = id[i] >= 0 && id[i] < a.rows;
     if (t < a.n && !valid && blockIdx.x == 0 && blockIdx.y == 0) raise_word(a.status);
-    const uint32_t row = (uint32_t)id / hop;
-    const bool mine = valid && (uint32_t)id - row * hop == blockIdx.x && id != a.padding;
+    const uint32_t row = (uint32_t)id[i] / hop;
+    const bool taken = valid && id[i] != a.padding, mine = taken && (uint32_t)id[i] - row * hop == blockIdx.x;
     const uint32_t ballot = __ballot_sync(0xffffffffu, mine);
-    int at = 0;
-    if (ballot != 0u && lane == 0) at = atomicAdd(&s_count, __popc(ballot));
-    at = __shfl_sync(0xffffffffu, at, 0);
-    if (mine) s_keys[at + __popc(ballot & ((1u << lane) - 1u))] = row << kDirectBits | (uint32_t)t;
-    if (valid && id >= z0 && id < z0 + rows && id != a.padding) s_seen[id - z0] = 1;
+    if (ballot != 0u) {
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&s_count, __popc(ballot));
+      at = __shfl_sync(0xffffffffu, at, 0);
+      if (mine) s_keys[at + __popc(ballot & ((1u << lane) - 1u))] = row << kDirectBits | (uint32_t)t;
+    }
+    if (taken && id[i] >= z0 && id[i] < z0 + rows) s_seen[id[i] - z0] = 1;
   }
   __syncthreads();
-  // all keys differ, so that any way to sort them gives the same order: rows, and in a row the tokens, ascending
+  // all keys differ, so that any way to sort them gives the same order: rows, and in a row the tokens, ascending.  Up to 256 a thread counts the keys below
+  // its own; more are sorted in a network.
   const int count = s_count;
-  int size = 32;
-  while (size < count) size <<= 1;
-  for (int i = count + tid; i < size && i < a.padded; i += kDirectThreads) s_keys[i] = 0xffffffffu;
-  __syncthreads();
-  if (count > 1) {
+  if (count <= 256) {
+    uint32_t mine = 0;
+    int below = 0;
+    const int quads = (count + 3) / 4;
+    if (tid >= count && tid < quads * 4) s_keys[tid] = 0xffffffffu;
+    __syncthreads();
+    if (tid < count) {
+      mine = s_keys[tid];
+      for (int q = 0; q < quads; ++q) {
+        const uint4 k = reinterpret_cast<const uint4*>(s_keys)[q];
+        below += (k.x < mine) + (k.y < mine) + (k.z < mine) + (k.w < mine);
+      }
+    }
+    __syncthreads();
+    if (tid < count) s_keys[below] = mine;
+    __syncthreads();
+  } else {
+    int size = 512;
+    while (size < count) size <<= 1;
+    for (int i = count + tid; i < size; i += kDirectThreads) s_keys[i] = 0xffffffffu;
+    __syncthreads();
     for (int k = 2; k <= size; k <<= 1) {
       for (int j = k >> 1; j > 0; j >>= 1) {
         for (int p = tid; p < size / 2; p += kDirectThreads) {
@@ -685,7 +708,7 @@ cudaError_t direct_typed(DirectArgs& a, cudaStream_t st) {
   int64_t ctas = std::max<int64_t>(1, std::min<int64_t>(a.rows, 2 * 148 / slabs));
   ctas = std::max({ctas, (a.rows + (int64_t)slabs * kDirectRows - 1) / ((int64_t)slabs * kDirectRows), (a.rows >> (32 - kDirectBits)) + 1});
   a.per = (int)((a.rows + ctas * slabs - 1) / (ctas * slabs));
-  a.padded = 32;
+  a.padded = 512;                                                // (the network's size, where it is used)
   while (a.padded < a.n) a.padded <<= 1;
   const size_t smem = (size_t)a.padded * 4 + (size_t)2 * kDirectWarps * COLS * 4 + (a.per + 3) / 4 * 4;
   emb_direct_kernel<T, VEC><<<dim3((unsigned)ctas, slabs), kDirectThreads, smem, st>>>(a);
@@ -739,10 +762,10 @@ int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
   if (b.n == 0 && b.accumulate) return (int)cudaSuccess;
   const EmbLayout l = emb_layout(b.n, b.cols);
   const int vec_out = reinterpret_cast<uintptr_t>(b.out) % 16 == 0 && b.ld_out % 4 == 0;
-  // One launch for up to 2048 tokens, and up to 4096 where the gradient is small.  Kernels alone, us, one launch | three (tokens x rows x columns, fp32):
-  // 1 x 50000 x 64 7 | 13, 256 x 21294 x 38 7 | 18, 1000 x 5000 x 64 8 | 22, 1000 x 32000 x 1024 29 | 32, 4001 x 10007 x 515 23 | 24, 4000 x 10000 x 512
-  // 22 | 22, 4000 x 32000 x 2048 69 | 60
-  if (b.n <= 2048 || (b.n <= kDirectMost && b.rows * b.cols <= (int64_t)1 << 23)) {
+  // One launch, or three.  Kernels alone, us, one | three (tokens x rows x columns, fp32): 1 x 50000 x 64 7 | 13, 256 x 21294 x 38 6 | 18,
+  // 1000 x 5000 x 64 6 | 22, 1000 x 32000 x 1024 27 | 32, 4001 x 10007 x 515 22 | 24, 4000 x 10000 x 512 21 | 22, 4000 x 32000 x 2048 59 | 60; longer lists, where
+  // a frequent id's tokens wait for one CTA: 8000 x 32000 x 512 42 | 26.
+  if (b.n <= kDirectMost) {
     DirectArgs d{};
     d.ids = Ids{b.ids, b.id_bytes == 8}; d.n = (int)b.n; d.rows = b.rows; d.cols = b.cols; d.padding = b.padding; d.dout = b.grad; d.ld = b.ld;
     d.scale = b.scale; d.accumulate = b.accumulate; d.out = b.out; d.ld_out = b.ld_out; d.vec_out = vec_out; d.status = b.status;

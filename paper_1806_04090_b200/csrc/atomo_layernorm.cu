@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(CTA, 512 / CTA) ln_forward_kernel(int group_wi
 template <typename T, int VEC, int PACKS, int CTA>
 __global__ void __launch_bounds__(CTA, 512 / CTA) ln_backward_kernel(int group_width, const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, int64_t rows, int cols,
                                                                 Weight weight, const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                                T* dx, int64_t ld_dx, float* __restrict__ parts) {
+                                                                T* dx, int64_t ld_dx, float* __restrict__ parts_w, float* __restrict__ parts_b) {
   constexpr int E = VEC * PACKS, R = rows_per_step(E * sizeof(T)), kStages = kBackwardStages;
   extern __shared__ uint4 s_ring[];                              // afterwards, of several groups: [groups][2][cols] floats
   __shared__ float2 s_sum[2][R][16];
@@ -403,8 +403,8 @@ __global__ void __launch_bounds__(CTA, 512 / CTA) ln_backward_kernel(int group_w
     low_x += (uint32_t)step_x * (uint32_t)sizeof(T); low_dy += (uint32_t)step_dy * (uint32_t)sizeof(T); to += step_dx;
   }
   // this CTA's rows of partial sums: dw, then db
-  float* part_w = parts + (int64_t)blockIdx.x * cols;
-  float* part_b = parts + ((int64_t)gridDim.x + blockIdx.x) * cols;
+  float* part_w = parts_w ? parts_w + (int64_t)blockIdx.x * cols : nullptr;        // (null: a result that is not asked for)
+  float* part_b = parts_b ? parts_b + (int64_t)blockIdx.x * cols : nullptr;
   if (beside > 1) {
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();                                             // the ring is no longer read
@@ -416,11 +416,12 @@ __global__ void __launch_bounds__(CTA, 512 / CTA) ln_backward_kernel(int group_w
     for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) {
       float t = 0.0f;
       for (int v = 0; v < beside; ++v) t += s_cols[v * 2 * cols + c];
-      if (c < cols) part_w[c] = t; else part_b[c - cols] = t;
+      float* part = c < cols ? part_w : part_b;
+      if (part) part[c < cols ? c : c - cols] = t;
     }
   } else {
-    put_columns<VEC, PACKS>(part_w, width, lane, in, dw);
-    put_columns<VEC, PACKS>(part_b, width, lane, in, db);
+    if (part_w) put_columns<VEC, PACKS>(part_w, width, lane, in, dw);
+    if (part_b) put_columns<VEC, PACKS>(part_b, width, lane, in, db);
   }
 }
 
@@ -620,11 +621,13 @@ cudaError_t backward_cta(const NormBackward& a, Shape s, cudaStream_t st) {
   const int beside = s.threads / s.width;
   const size_t smem = std::max<size_t>(Ring<T, VEC, PACKS, 2 * R, kBackwardStages, CTA>::bytes(beside, (int)a.cols), beside > 1 ? (size_t)beside * 2 * a.cols * 4 : 0);
   static int known[17];
-  const int grid = std::min(back_ctas(a.rows, (int64_t)beside * R), resident((const void*)ln_backward_kernel<T, VEC, PACKS, CTA>, s.threads, smem, known));
+  // a few steps: one CTA, whose sums are the results (the join is a launch, and 3 us)
+  const bool one = a.rows <= 4 * beside * R;
+  const int grid = one ? 1 : std::min(back_ctas(a.rows, (int64_t)beside * R), resident((const void*)ln_backward_kernel<T, VEC, PACKS, CTA>, s.threads, smem, known));
   ln_backward_kernel<T, VEC, PACKS, CTA><<<grid, s.threads, smem, st>>>(s.width, (const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, a.rows, (int)a.cols, Weight{a.weight, a.weight_type}, a.mean, a.rstd,
-                                                                        (T*)a.dx, a.ld_dx, a.ws);
+                                                                        (T*)a.dx, a.ld_dx, one ? a.dweight : a.ws, one ? a.dbias : a.ws + (int64_t)grid * a.cols);
   const cudaError_t e = cudaGetLastError();
-  return e != cudaSuccess ? e : backward_join(a, grid, st);
+  return e != cudaSuccess || one ? e : backward_join(a, grid, st);
 }
 template <typename T, int VEC, int PACKS>
 cudaError_t backward_form(const NormBackward& a, cudaStream_t st) {
