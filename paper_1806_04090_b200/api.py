@@ -449,6 +449,9 @@ class Atomo:
         self._ew_format, self._ew_sat_cap = EW_EXPLICIT, 0
         if rc != 0:
             raise AtomoError(rc, "atomo_create", self._cuda_error())
+        # tensors that new ones are made after (cheaper than naming type and device each time)
+        self._floats = torch.empty(1, dtype=torch.float32, device=self._torch_device)
+        self._bytes = torch.empty(1, dtype=torch.uint8, device=self._torch_device)
 
     def _cuda_error(self) -> str:
         try:
@@ -644,20 +647,20 @@ class Atomo:
 
     # ---- operators on either side of the exchange ---------------------------------------------
     # (Small calls take as long as their host side: what is a C call on a tensor, an allocation or a ctypes object is counted here.)
-    def _own_stream(self, stream: Optional[torch.cuda.Stream]) -> int:
-        """The stream given, or the current one of the context's device (whatever device is current)."""
-        if stream is None:
-            return torch._C._cuda_getCurrentRawStream(self.device)
+    def _on(self, stream: torch.cuda.Stream, call, *args):
+        """A call with `stream` current, so that what it allocates belongs to that stream too."""
         if stream.device_index != self.device:
             raise ValueError(f"the stream belongs to device {stream.device_index}, the context to device {self.device}")
-        return stream.cuda_stream
+        with torch.cuda.stream(stream):
+            return call(*args)
 
-    def _scratch(self, nbytes: int, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
-        """A workspace for one call: torch's allocator keeps it from other work of this stream's order, also in a captured graph."""
-        t = torch.empty(nbytes, dtype=torch.uint8, device=self._torch_device)
-        if stream is not None:
-            t.record_stream(stream)
-        return t
+    def _own_stream(self) -> int:
+        """The current stream of the context's device (whatever device is current)."""
+        return torch._C._cuda_getCurrentRawStream(self.device)
+
+    def _scratch(self, nbytes: int) -> torch.Tensor:
+        """A workspace for one call: torch's allocator keeps it from other work until this stream is done with it, also in a captured graph."""
+        return self._bytes.new_empty(nbytes)
 
     def _operand(self, t, what: str, types=TYPE_CODES) -> torch.Tensor:
         if not (isinstance(t, torch.Tensor) and t.get_device() == self.device and t.dtype in types):
@@ -668,6 +671,8 @@ class Atomo:
                         stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """Two fp32 numbers on the device: the 2-norm over all elements of all gradients, and min(1, max_norm / (norm + 1e-6)), the factor
         that clips them (NaN where the norm is not finite), as atomo_adamw takes them.  Gradients: contiguous fp32, bf16 or fp16."""
+        if stream is not None:
+            return self._on(stream, self.atomo_grad_norm, grads, max_norm, out)
         device, codes = self.device, TYPE_CODES
         desc = []                                        # of _Tensor
         for g in grads:
@@ -677,15 +682,15 @@ class Atomo:
             desc += (g.data_ptr(), g.numel(), code)
         n = len(desc) // 3
         if out is None:
-            out = torch.empty(2, dtype=torch.float32, device=self._torch_device)
+            out = self._floats.new_empty(2)
         elif not (out.get_device() == device and out.dtype == torch.float32 and out.numel() == 2 and out.is_contiguous()):
             raise ValueError(f"out: two fp32 numbers on CUDA device {device} are required")
-        s = self._own_stream(stream)
+        s = self._own_stream()
         packed = struct.pack("=" + "qqq" * n, *desc)     # (the type's high half is the reserved word)
         nbytes = self.lib.atomo_grad_norm_workspace_bytes(packed, n)
         if nbytes < 0:
             raise AtomoError(1, "atomo_grad_norm_workspace_bytes")
-        ws = self._scratch(nbytes, stream) if nbytes else None
+        ws = self._scratch(nbytes) if nbytes else None
         self._check(self.lib.atomo_grad_norm(self._h, packed, n, max_norm, out.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, s), "atomo_grad_norm")
         return out
 
@@ -694,6 +699,8 @@ class Atomo:
         """One AdamW step (decoupled weight decay) over all parameters of `state`, in place.  grads: one contiguous tensor per parameter, all of
         one type.  step counts from 1.  scale: what atomo_grad_norm returned; its second number multiplies the gradients, and where it
         is not finite nothing is updated.  seed: of the stochastic rounding of 8-bit states."""
+        if stream is not None:
+            return self._on(stream, self.atomo_adamw, state, grads, lr, step, beta1, beta2, eps, seed, scale)
         n, device = len(state.lengths), self.device
         if len(grads) != n:
             raise ValueError(f"{n} gradients are required")
@@ -710,7 +717,7 @@ class Atomo:
         if scale is not None and not (scale.get_device() == device and scale.dtype == torch.float32 and scale.numel() == 2 and scale.is_contiguous()):
             raise ValueError(f"scale: two fp32 numbers on CUDA device {device} are required")
         args = _ADAMW_ARGS(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, 0 if scale is None else scale.data_ptr(), state.bits, TYPE_CODES[kind])
-        rc = self.lib.atomo_adamw(self._h, state._desc, struct.pack("=%dQ" % n, *ptrs), n, args, self._own_stream(stream))
+        rc = self.lib.atomo_adamw(self._h, state._desc, struct.pack("=%dQ" % n, *ptrs), n, args, self._own_stream())
         self._check(rc, "atomo_adamw")
 
     def _status(self, status: Optional[torch.Tensor]):
@@ -729,6 +736,8 @@ class Atomo:
                         status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """scale * table[ids], of shape ids.shape + (cols,).  An id outside the table gives a row of zeros and raises `status` (one int32, set to
         zero by the caller) to ATOMO_ERR_INVALID_ARG."""
+        if stream is not None:
+            return self._on(stream, self.atomo_embedding, table, ids, scale, out, status)
         kind = self._operand(table, "table").dtype
         if table.dim() != 2:
             raise ValueError("table: a matrix is required")
@@ -744,7 +753,7 @@ class Atomo:
             if n_out != n:
                 raise ValueError(f"out: {n} rows are required")
         rc = self.lib.atomo_embedding(self._h, table.data_ptr(), TYPE_CODES[kind], rows, cols, ld, ids.data_ptr(), width, n, scale, out.data_ptr(), ld_out,
-                                      self._status(status) if status is not None else None, self._own_stream(stream))
+                                      self._status(status) if status is not None else None, self._own_stream())
         self._check(rc, "atomo_embedding")
         return out
 
@@ -753,6 +762,8 @@ class Atomo:
                                  stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """The gradient of a table of `rows` rows, fp32: row v is scale times the sum of grad over the tokens of id v, in the order of the
         tokens.  grad: ids.shape + (cols,).  out: a matrix to write to, or with accumulate=True to add to.  Tokens of padding_idx (-1: none) are left out."""
+        if stream is not None:
+            return self._on(stream, self.atomo_embedding_backward, ids, grad, rows, scale, padding_idx, out, accumulate, status)
         code = TYPE_CODES[self._operand(grad, "grad").dtype]
         width = self._ids(ids)
         if grad.dim() < 1 or grad.shape[:-1] != ids.shape:
@@ -762,19 +773,19 @@ class Atomo:
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs out")
-            out = torch.empty(rows, cols, dtype=torch.float32, device=self._torch_device)
+            out = self._floats.new_empty((rows, cols))
             ld_out = cols
         else:
             n_out, ld_out = _rows(self._operand(out, "out", (torch.float32,)), cols, "out")
             if n_out != rows:
                 raise ValueError(f"out: {rows} rows are required")
-        s = self._own_stream(stream)
+        s = self._own_stream()
         nbytes = self.lib.atomo_embedding_workspace_bytes(n, rows, cols)
         if nbytes < 0:
             raise AtomoError(1, "atomo_embedding_workspace_bytes")
-        ws = self._scratch(nbytes, stream)
+        ws = self._scratch(nbytes) if nbytes else None
         rc = self.lib.atomo_embedding_backward(self._h, ids.data_ptr(), width, n, grad.data_ptr(), code, ld, rows, cols, scale, padding_idx, out.data_ptr(), ld_out,
-                                               1 if accumulate else 0, self._status(status), ws.data_ptr(), nbytes, s)
+                                               1 if accumulate else 0, self._status(status), ws.data_ptr() if nbytes else None, nbytes, s)
         self._check(rc, "atomo_embedding_backward")
         return out
 
@@ -791,6 +802,8 @@ class Atomo:
                          out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
         """Layer norm over the last dimension: (y, mean, rstd), y of x's type and shape, mean and rstd in fp32 with one value per row.  out may
         be x."""
+        if stream is not None:
+            return self._on(stream, self.atomo_layer_norm, x, weight, bias, eps, out)
         kind = self._operand(x, "x").dtype
         shape = x.shape
         cols = shape[-1] if shape else 0
@@ -806,10 +819,9 @@ class Atomo:
                 raise ValueError("out: the shape of x is required")
             ld_out = cols if out.is_contiguous() else _rows(out, cols, "out")[1]
         lines = rows if len(shape) == 2 else shape[:-1]
-        mean = torch.empty(lines, dtype=torch.float32, device=self._torch_device)
-        rstd = torch.empty(lines, dtype=torch.float32, device=self._torch_device)
+        mean, rstd = self._floats.new_empty(lines), self._floats.new_empty(lines)
         rc = self.lib.atomo_layer_norm(self._h, x.data_ptr(), TYPE_CODES[kind], rows, cols, ld, w, b, TYPE_CODES[wkind or bkind or kind], eps, out.data_ptr(), ld_out,
-                                       mean.data_ptr(), rstd.data_ptr(), self._own_stream(stream))
+                                       mean.data_ptr(), rstd.data_ptr(), self._own_stream())
         self._check(rc, "atomo_layer_norm")
         return out, mean, rstd
 
@@ -817,6 +829,8 @@ class Atomo:
                                   out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
         """(dx, dweight, dbias) of atomo_layer_norm: dx of x's type, dweight and dbias in fp32, whatever the weight's type.  out (for dx) may
         be dy or x."""
+        if stream is not None:
+            return self._on(stream, self.atomo_layer_norm_backward, dy, x, weight, mean, rstd, out)
         kind = self._operand(x, "x").dtype
         self._operand(dy, "dy", (kind,))
         shape = x.shape
@@ -835,15 +849,14 @@ class Atomo:
             if self._operand(out, "out", (kind,)).shape != shape:
                 raise ValueError("out: the shape of x is required")
             ld_dx = cols if out.is_contiguous() else _rows(out, cols, "out")[1]
-        dweight = torch.empty(cols, dtype=torch.float32, device=self._torch_device)
-        dbias = torch.empty(cols, dtype=torch.float32, device=self._torch_device)
-        s = self._own_stream(stream)
+        dweight, dbias = self._floats.new_empty(cols), self._floats.new_empty(cols)
+        s = self._own_stream()
         nbytes = self.lib.atomo_layer_norm_workspace_bytes(rows, cols)
         if nbytes < 0:
             raise AtomoError(1, "atomo_layer_norm_workspace_bytes")
-        ws = self._scratch(nbytes, stream)
+        ws = self._scratch(nbytes) if nbytes else None
         rc = self.lib.atomo_layer_norm_backward(self._h, dy.data_ptr(), ld_dy, x.data_ptr(), ld, TYPE_CODES[kind], rows, cols, w, TYPE_CODES[wkind or kind], mean.data_ptr(), rstd.data_ptr(),
-                                                out.data_ptr(), ld_dx, dweight.data_ptr(), dbias.data_ptr(), ws.data_ptr(), nbytes, s)
+                                                out.data_ptr(), ld_dx, dweight.data_ptr(), dbias.data_ptr(), ws.data_ptr() if nbytes else None, nbytes, s)
         self._check(rc, "atomo_layer_norm_backward")
         return out, dweight, dbias
 

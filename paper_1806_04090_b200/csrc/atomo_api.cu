@@ -1567,7 +1567,7 @@ int atomo_embedding_backward(atomo_ctx* ctx, const void* ids, int32_t id_bytes, 
   if (!std::isfinite(scale) || bad_ptr(out, 4) || off_type(status, 4) || padding_idx < -1 || padding_idx >= rows) return ATOMO_ERR_INVALID_ARG;
   if (n_ids > 0 && (bad_ptr(ids, id_bytes) || bad_ptr(grad, type_bytes(type)))) return ATOMO_ERR_INVALID_ARG;
   const int64_t need = atomo_embedding_workspace_bytes(n_ids, rows, cols);
-  if (bad_ptr(workspace, 16)) return ATOMO_ERR_INVALID_ARG;
+  if (need > 0 && bad_ptr(workspace, 16)) return ATOMO_ERR_INVALID_ARG;
   if (workspace_bytes < need) return ATOMO_ERR_CAPACITY;
   const EmbBackward a{ids, id_bytes, n_ids, grad, type, ld, rows, cols, (float)scale, padding_idx, out, ld_out, accumulate != 0, status, static_cast<uint8_t*>(workspace)};
   return on_device(ctx, "embedding gradient", [&] { return launch_embedding_backward(a, (cudaStream_t)stream); });
@@ -1593,8 +1593,10 @@ int atomo_layer_norm_backward(atomo_ctx* ctx, const void* dy, int64_t ld_dy, con
   if (!ctx || bad_type(type) || bad_type(weight_type) || rows > kNormRows || bad_shape(rows, cols, ld_dy) || bad_shape(rows, cols, ld_x) || bad_shape(rows, cols, ld_dx)) return ATOMO_ERR_INVALID_ARG;
   if (off_type(weight, type_bytes(weight_type)) || off_type(dweight, 4) || off_type(dbias, 4)) return ATOMO_ERR_INVALID_ARG;
   const int size = type_bytes(type);
-  if (rows > 0 && (bad_ptr(dy, size) || bad_ptr(x, size) || bad_ptr(dx, size) || bad_ptr(mean, 4) || bad_ptr(rstd, 4) || bad_ptr(workspace, 16))) return ATOMO_ERR_INVALID_ARG;
-  if (workspace_bytes < atomo_layer_norm_workspace_bytes(rows, cols)) return ATOMO_ERR_CAPACITY;
+  if (rows > 0 && (bad_ptr(dy, size) || bad_ptr(x, size) || bad_ptr(dx, size) || bad_ptr(mean, 4) || bad_ptr(rstd, 4))) return ATOMO_ERR_INVALID_ARG;
+  const int64_t need = atomo_layer_norm_workspace_bytes(rows, cols);
+  if (need > 0 && bad_ptr(workspace, 16)) return ATOMO_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return ATOMO_ERR_CAPACITY;
   const NormBackward a{dy, x, type, rows, cols, ld_dy, ld_x, weight, weight_type, mean, rstd, dx, ld_dx, dweight, dbias, static_cast<float*>(workspace)};
   return on_device(ctx, "layer norm gradient", [&] { return launch_layer_norm_backward(a, (cudaStream_t)stream); });
 }

@@ -756,11 +756,10 @@ int launch_embedding(const EmbLookup& a, cudaStream_t st) {
   return (int)lookup_type<__half>(a, st);
 }
 
-uint64_t embedding_workspace(int64_t n, int64_t cols) { return emb_layout(n, cols).bytes; }
+uint64_t embedding_workspace(int64_t n, int64_t cols) { return n <= kDirectMost ? 0 : emb_layout(n, cols).bytes; }
 
 int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
   if (b.n == 0 && b.accumulate) return (int)cudaSuccess;
-  const EmbLayout l = emb_layout(b.n, b.cols);
   const int vec_out = reinterpret_cast<uintptr_t>(b.out) % 16 == 0 && b.ld_out % 4 == 0;
   // One launch, or three.  Kernels alone, us, one | three (tokens x rows x columns, fp32): 1 x 50000 x 64 7 | 13, 256 x 21294 x 38 6 | 18,
   // 1000 x 5000 x 64 6 | 22, 1000 x 32000 x 1024 27 | 32, 4001 x 10007 x 515 22 | 24, 4000 x 10000 x 512 21 | 22, 4000 x 32000 x 2048 59 | 60; longer lists, where
@@ -771,6 +770,7 @@ int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
     d.scale = b.scale; d.accumulate = b.accumulate; d.out = b.out; d.ld_out = b.ld_out; d.vec_out = vec_out; d.status = b.status;
     return (int)(b.type == ATOMO_TYPE_F32 ? direct_type<float>(d, st) : b.type == ATOMO_TYPE_BF16 ? direct_type<__nv_bfloat16>(d, st) : direct_type<__half>(d, st));
   }
+  const EmbLayout l = emb_layout(b.n, b.cols);
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return (int)e;
@@ -795,14 +795,14 @@ int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
   const size_t smem = s.segment <= kSortTile ? kSortTile * 16 : kSortTile * 8;
   const SortLaunch launch(ctas, (int)(ctas + others), smem, st);
   e = s.segment <= kSortTile ? cudaLaunchKernelEx(&launch.cfg, emb_sort_kernel<true>, s) : cudaLaunchKernelEx(&launch.cfg, emb_sort_kernel<false>, s);
-  if (e != cudaSuccess || b.n == 0) return (int)e;
+  if (e != cudaSuccess) return (int)e;
   SumArgs a{};
   a.items = s.items[s.passes & 1]; a.runs = s.runs;
   a.n = b.n; a.chunks = l.chunks; a.rows = b.rows; a.cols = b.cols;
   a.dout = b.grad; a.ld = b.ld; a.scale = b.scale; a.accumulate = b.accumulate; a.out = b.out; a.ld_out = b.ld_out; a.vec_out = vec_out;
   a.parts = reinterpret_cast<float*>(b.ws + l.parts); a.ld_part = l.ld_part;
   e = b.type == ATOMO_TYPE_F32 ? sum_type<float>(a, st) : b.type == ATOMO_TYPE_BF16 ? sum_type<__nv_bfloat16>(a, st) : sum_type<__half>(a, st);
-  if (e != cudaSuccess || l.chunks < 3) return (int)e;           // no run of fewer chunks is long
+  if (e != cudaSuccess) return (int)e;
   const int64_t units = (l.chunks / 2) * ((b.cols + 127) / 128);
   return (int)launch_after(emb_join_kernel, dim3((unsigned)std::min<int64_t>(units, 148 * 8)), dim3(32, kJoinSlices), 0, st, a);
 }

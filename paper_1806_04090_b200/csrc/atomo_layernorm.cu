@@ -680,7 +680,10 @@ int launch_layer_norm(const NormForward& a, cudaStream_t st) {
   return (int)forward_type<__half>(a, st);
 }
 
-uint64_t layer_norm_workspace(int64_t rows, int64_t cols) { return (uint64_t)std::min<int64_t>(rows, kBackCtas) * 2 * cols * 4; }
+uint64_t layer_norm_workspace(int64_t rows, int64_t cols) {
+  if (rows <= 4 && cols <= kNormCols) return 0;                  // one CTA, whatever the type
+  return (uint64_t)std::min<int64_t>(rows, kBackCtas) * 2 * cols * 4;
+}
 
 int launch_layer_norm_backward(const NormBackward& a, cudaStream_t st) {
   if (a.type == ATOMO_TYPE_F32) return (int)backward_type<float>(a, st);

@@ -67,16 +67,16 @@ def test_embedding(ctx):
         assert look(**bad) == INVALID, bad
 
     size = lib.atomo_embedding_workspace_bytes
-    assert size(3, 8, 4) > 0 and size(0, 8, 4) >= 0
+    assert size(3, 8, 4) == size(0, 8, 4) == 0 and size(100000, 8, 4) > 0
     assert size(-1, 8, 4) == size(3, 0, 4) == size(3, 8, 0) == size(1 << 31, 8, 4) == size(3, 1 << 31, 4) == -1
 
     def back(ids=GOOD, width=8, n=3, grad=GOOD, kind=0, ld=4, rows=8, cols=4, scale=1.0, padding=-1, out=GOOD, ld_out=4, status=None, ws=GOOD, nbytes=1 << 30):
         return lib.atomo_embedding_backward(h, ids, width, n, grad, kind, ld, rows, cols, scale, padding, out, ld_out, 0, status, ws, nbytes, None)
 
     for bad in (dict(ids=None), dict(ids=GOOD + 4), dict(width=1), dict(n=-1), dict(grad=None), dict(grad=GOOD + 2), dict(kind=-1), dict(ld=3), dict(rows=0), dict(cols=0), dict(scale=float("inf")),
-                dict(padding=-2), dict(padding=8), dict(out=None), dict(out=GOOD + 2), dict(ld_out=3), dict(status=GOOD + 2), dict(ws=None), dict(ws=GOOD + 8)):
+                dict(padding=-2), dict(padding=8), dict(out=None), dict(out=GOOD + 2), dict(ld_out=3), dict(status=GOOD + 2), dict(n=100000, ws=None), dict(n=100000, ws=GOOD + 8)):
         assert back(**bad) == INVALID, bad
-    assert back(nbytes=size(3, 8, 4) - 1) == CAPACITY
+    assert back(n=100000, nbytes=size(100000, 8, 4) - 1) == CAPACITY
 
 
 def test_layer_norm(ctx):
@@ -90,15 +90,15 @@ def test_layer_norm(ctx):
         assert forward(**bad) == INVALID, bad
 
     size = lib.atomo_layer_norm_workspace_bytes
-    assert size(3, 4) > 0 and size(-1, 4) == size(3, 0) == -1
+    assert size(3, 4) == 0 and size(100, 4) > 0 and size(3, 100000) > 0 and size(-1, 4) == size(3, 0) == size((1 << 30) + 1, 4) == -1
 
     def backward(dy=GOOD, ld_dy=4, x=GOOD, ld_x=4, kind=0, rows=3, cols=4, w=GOOD, wkind=0, mean=GOOD, rstd=GOOD, dx=GOOD, ld_dx=4, dw=GOOD, db=GOOD, ws=GOOD, nbytes=1 << 30):
         return lib.atomo_layer_norm_backward(h, dy, ld_dy, x, ld_x, kind, rows, cols, w, wkind, mean, rstd, dx, ld_dx, dw, db, ws, nbytes, None)
 
     for bad in (dict(dy=None), dict(ld_dy=3), dict(x=None), dict(x=GOOD + 2), dict(ld_x=3), dict(kind=4), dict(rows=-1), dict(cols=0), dict(w=GOOD + 2), dict(wkind=-1), dict(mean=None),
-                dict(rstd=GOOD + 2), dict(dx=None), dict(ld_dx=2), dict(dw=GOOD + 2), dict(db=GOOD + 1), dict(ws=None), dict(ws=GOOD + 4)):
+                dict(rstd=GOOD + 2), dict(dx=None), dict(ld_dx=2), dict(dw=GOOD + 2), dict(db=GOOD + 1), dict(rows=100, ws=None), dict(rows=100, ws=GOOD + 4)):
         assert backward(**bad) == INVALID, bad
-    assert backward(nbytes=size(3, 4) - 1) == CAPACITY
+    assert backward(rows=100, nbytes=size(100, 4) - 1) == CAPACITY
 
 
 def test_adamw_state_checks_its_tensors():
