@@ -3,11 +3,11 @@
 //   out[t] = s table[id[t]],   dtable[v] = s sum_{t : id[t] = v} dout[t]
 //
 // The gradient's sums run in the order of the tokens, so that the same call gives the same bits each time (a payload that is encoded
-// from it does too), which sums by atomics would not.  Three kernels:
+// from it does too), which sums by atomics would not.  Four kernels:
 //   emb_sort_kernel   stable radix sort of (id, token), eight bits a pass, by the CTAs of one cluster: they exchange their histograms
 //                     through distributed shared memory and their items through L2, with the hardware cluster barrier between; a tile's items are put in
-//                     order in shared memory first, so that they leave in runs.  It also lists the long runs of equal ids.  Meanwhile the launch's other CTAs write the rows
-//                     without tokens: each looks through the ids for those of its own rows, so that none of them waits for the sort.
+//                     order in shared memory first, so that they leave in runs.  It also lists the long runs of equal ids.
+//   emb_zero_kernel   writes the rows without tokens, beside the sort: a CTA looks through the ids for those of its own rows, so that it needs no sort.
 //   emb_sum_kernel    chunks of kEmbChunk neighbouring sorted tokens, so that a frequent token's run is split among CTAs.  A run that ends in the chunk it
 //                     starts in, or in the next one, is summed by the former and goes to its row; a longer one leaves one part per chunk in the workspace.
 //   emb_join_kernel   adds the parts of the longer runs, in order.
@@ -95,9 +95,12 @@ struct SortArgs {
   int32_t* status;
   int passes, bits;
   int64_t segment;                      // tokens of a CTA
-  uint32_t ctas;                        // CTAs that sort: the first cluster.  The others write rows without tokens:
-  float* out; int64_t cols, ld_out; int vec_out;
+  uint32_t ctas;                        // CTAs: one cluster
+  int beside;                           // the next kernel in the stream runs beside this one
 };
+// rows without tokens
+struct ZeroArgs { Ids ids; int64_t n, rows, padding, cols; float* out; int64_t ld_out; int vec_out, wide_ids; };
+constexpr int kZeroThreads = 1024;
 
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -135,27 +138,34 @@ __device__ __forceinline__ void zero_row(float* p, int64_t cols, int vec) {
   }
   for (; c < cols; c += 32) p[c] = 0.0f;
 }
-// rows without tokens, by the CTAs behind those that sort: a range of rows each
-__device__ __forceinline__ void zero_rows(const SortArgs& a, uint8_t* s_seen) {
-  constexpr int64_t kFlags = 65536;
-  const int64_t per = (a.rows + (gridDim.x - a.ctas) - 1) / (gridDim.x - a.ctas);
-  const int64_t begin = (int64_t)(blockIdx.x - a.ctas) * per, end = min(begin + per, a.rows);
+// A range of rows per CTA.  It follows the sort in the stream, runs beside it (on the other SMs: a CTA that sorts takes all registers of its own) and ends after it.
+__global__ void __launch_bounds__(kZeroThreads, 2) emb_zero_kernel(const __grid_constant__ ZeroArgs a) {
+  constexpr int kFlags = 32768;
+  __shared__ uint8_t s_seen[kFlags];
+  const int64_t per = (a.rows + gridDim.x - 1) / gridDim.x, begin = (int64_t)blockIdx.x * per, end = min(begin + per, a.rows);
   for (int64_t r0 = begin; r0 < end; r0 += kFlags) {
-    const int64_t count = min(kFlags, end - r0);
-    for (int64_t i = threadIdx.x; i < count; i += kSortThreads) s_seen[i] = 0;
+    const int count = (int)min((int64_t)kFlags, end - r0);
+    for (int i = threadIdx.x; i < count; i += kZeroThreads) s_seen[i] = 0;
     __syncthreads();
+    auto see = [&](int64_t id) { if (id >= r0 && id < r0 + count && id != a.padding) s_seen[id - r0] = 1; };
+    int64_t done = 0;                                            // ids 16 bytes at a time, as far as they lie so
+    if (a.wide_ids) {
+      const int each = a.ids.wide ? 2 : 4;
+      const int64_t quads = a.n / each;
 #pragma unroll 8
-    for (int64_t t = threadIdx.x; t < a.n; t += kSortThreads) {
-      const int64_t id = load_id(a.ids, t);
-      if (id >= r0 && id < r0 + count && id != a.padding) s_seen[id - r0] = 1;
+      for (int64_t q = threadIdx.x; q < quads; q += kZeroThreads) {
+        const int4 v = reinterpret_cast<const int4*>(a.ids.p)[q];
+        if (a.ids.wide) { see((int64_t)v.y << 32 | (uint32_t)v.x); see((int64_t)v.w << 32 | (uint32_t)v.z); }
+        else { see(v.x); see(v.y); see(v.z); see(v.w); }
+      }
+      done = quads * each;
     }
+    for (int64_t t = done + threadIdx.x; t < a.n; t += kZeroThreads) see(load_id(a.ids, t));
     __syncthreads();
-    for (int64_t r = threadIdx.x >> 5; r < count; r += kSortWarps) {
-      if (s_seen[r]) continue;
-      zero_row(a.out + (r0 + r) * a.ld_out, a.cols, a.vec_out);
-    }
+    for (int r = threadIdx.x >> 5; r < count; r += kZeroThreads / 32) if (!s_seen[r]) zero_row(a.out + (r0 + r) * a.ld_out, a.cols, a.vec_out);
     __syncthreads();
   }
+  wait_for_previous();                   // so that what follows this kernel follows the sort too
 }
 
 // ONE: a CTA's segment fits one tile: its items stay in registers between ranking and writing, and between passes in the shared memory of the CTAs that
@@ -169,7 +179,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) emb_sort_kernel(const __grid_
   __shared__ uint32_t s_hist[256], s_base[256], s_tile[256], s_first[256], s_scan[2][8];   // s_first: of a digit in the ordered tile
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int64_t begin = min((int64_t)blockIdx.x * a.segment, a.n), end = min(begin + a.segment, a.n);
-  if (blockIdx.x >= a.ctas) return zero_rows(a, reinterpret_cast<uint8_t*>(s_items));
+  if (a.beside) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (blockIdx.x == 0 && tid == 0) a.runs[0] = 0;
   uint64_t item[kSortItems];
   uint32_t rank[kSortItems];
@@ -218,7 +228,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) emb_sort_kernel(const __grid_
       __syncthreads();
       if (tid < 256) {
         uint32_t run = 0;
-#pragma unroll
+#pragma unroll 16
         for (int w = 0; w < kSortWarps; ++w) { const uint32_t c = s_warp[w][tid]; s_warp[w][tid] = (uint16_t)run; run += c; }
         s_tile[tid] = run;
       }
@@ -424,10 +434,11 @@ __global__ void __launch_bounds__(kEmbThreads, 4) emb_sum_kernel(const __grid_co
   flush(part ? 0 : tail_part ? 1 : -1);
 }
 
-// A CTA adds the parts of one long run for 128 columns: eight slices of the run's chunks, then the slices.
-constexpr int kJoinSlices = 8;
+// A CTA adds the parts of one long run for 128 columns: eight slices of the run's chunks, then the slices.  A thread copies ten parts at a time to shared memory
+// asynchronously (of loads to registers the compiler kept one under way: 20 k cycles for a run of 294 chunks, 21 us in all).
+constexpr int kJoinSlices = 8, kJoinAhead = 10;
 __global__ void __launch_bounds__(32 * kJoinSlices) emb_join_kernel(const __grid_constant__ SumArgs a) {
-  __shared__ float4 s_part[kJoinSlices][32];
+  __shared__ float4 s_part[kJoinSlices][32], s_ahead[kJoinAhead][kJoinSlices][32];
   wait_for_previous();
   const int64_t slabs = (a.cols + 127) / 128, units = (int64_t)a.runs[0] * slabs;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
@@ -444,10 +455,12 @@ __global__ void __launch_bounds__(32 * kJoinSlices) emb_join_kernel(const __grid
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (col < a.cols) {
       const int64_t i1 = min(count, (threadIdx.y + 1) * per);
-#pragma unroll 8
-      for (int64_t i = threadIdx.y * per; i < i1; ++i) {
-        const float4 x = *reinterpret_cast<const float4*>(a.parts + ((c0 + i) * 2 + (i == 0 ? 1 : 0)) * a.ld_part + col);
-        acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
+      const float* p = a.parts + c0 * 2 * a.ld_part + col;       // slot 1 of the first chunk, slot 0 of the others
+      for (int64_t i = threadIdx.y * per; i < i1; i += kJoinAhead) {
+        const int n = (int)min((int64_t)kJoinAhead, i1 - i);
+        for (int u = 0; u < n; ++u) copy_async<16>(&s_ahead[u][threadIdx.y][threadIdx.x], p + ((i + u) * 2 + (i + u == 0)) * a.ld_part);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        for (int u = 0; u < n; ++u) { const float4 x = s_ahead[u][threadIdx.y][threadIdx.x]; acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w; }
       }
     }
     s_part[threadIdx.y][threadIdx.x] = acc;
@@ -675,10 +688,10 @@ struct SortRoom { int clusters[5]; } sort_room[64];
 struct SortLaunch {
   cudaLaunchAttribute attr[1];
   cudaLaunchConfig_t cfg = {};
-  SortLaunch(int cluster, int grid, size_t smem, cudaStream_t st) {
+  SortLaunch(int cluster, size_t smem, cudaStream_t st) {
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(kSortThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 1;
+    cfg.gridDim = dim3(cluster); cfg.blockDim = dim3(kSortThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 1;
   }
   SortLaunch(const SortLaunch&) = delete;
 };
@@ -741,7 +754,7 @@ int embedding_configure(int device) {
                     cudaFuncSetAttribute(emb_sort_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
   for (int lg = 0; lg <= 4; ++lg) {
     int clusters = 0;
-    const SortLaunch l(1 << lg, 1 << lg, kSortTile * 16, nullptr);
+    const SortLaunch l(1 << lg, kSortTile * 16, nullptr);
     if ((lg < 4 || wide) && cudaOccupancyMaxActiveClusters(&clusters, emb_sort_kernel<true>, &l.cfg) != cudaSuccess) clusters = 0;
     sort_room[device & 63].clusters[lg] = clusters;
   }
@@ -778,7 +791,6 @@ int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
   s.ids = Ids{b.ids, b.id_bytes == 8}; s.n = b.n; s.rows = b.rows; s.padding = b.padding; s.status = b.status;
   for (int i = 0; i < 2; ++i) s.items[i] = reinterpret_cast<uint64_t*>(b.ws + l.items[i]);
   s.runs = reinterpret_cast<uint32_t*>(b.ws + l.runs);
-  s.out = b.out; s.cols = b.cols; s.ld_out = b.ld_out; s.vec_out = vec_out;
   int bits = 1;
   while ((b.rows >> bits) != 0) ++bits;                          // ids as sort keys are 0 .. rows
   s.passes = (bits + 7) / 8; s.bits = (bits + s.passes - 1) / s.passes;
@@ -789,12 +801,14 @@ int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
   const int ctas = 1 << lg;
   s.ctas = (uint32_t)ctas;
   s.segment = (b.n + ctas - 1) / ctas;
-  // the clusters that run beside it, for the rows without tokens; fewer where a CTA would have less than 16 KB of them
-  const int64_t most = b.accumulate ? 0 : std::max<int64_t>(1, b.rows * b.cols / 4096);
-  const int64_t others = std::min<int64_t>(std::max(1, room.clusters[lg] - 1), (most + ctas - 1) / ctas) * ctas;
+  s.beside = !b.accumulate;
   const size_t smem = s.segment <= kSortTile ? kSortTile * 16 : kSortTile * 8;
-  const SortLaunch launch(ctas, (int)(ctas + others), smem, st);
+  const SortLaunch launch(ctas, smem, st);
   e = s.segment <= kSortTile ? cudaLaunchKernelEx(&launch.cfg, emb_sort_kernel<true>, s) : cudaLaunchKernelEx(&launch.cfg, emb_sort_kernel<false>, s);
+  if (e == cudaSuccess && s.beside) {    // a CTA on each of the other SMs, fewer where one would have less than 16 KB to write
+    const ZeroArgs z{s.ids, b.n, b.rows, b.padding, b.cols, b.out, b.ld_out, vec_out, reinterpret_cast<uintptr_t>(b.ids) % 16 == 0};
+    e = launch_after(emb_zero_kernel, dim3((unsigned)std::min<int64_t>(148 - ctas, std::max<int64_t>(1, b.rows * b.cols / 4096))), dim3(kZeroThreads), 0, st, z);
+  }
   if (e != cudaSuccess) return (int)e;
   SumArgs a{};
   a.items = s.items[s.passes & 1]; a.runs = s.runs;
