@@ -319,7 +319,7 @@ int atomo_adamw(atomo_ctx* ctx, const atomo_adamw_tensor* tensors /*HOST array*/
  * Backward: out[v] = scale * sum of grad[t] over the tokens t with ids[t] = v, in the order of the tokens; out is fp32, every
  * element of its rows x cols is written (accumulate != 0: added to what is there).  grad is n_ids x cols of `type`, leading dimension ld.  Tokens whose id
  * is padding_idx (-1: none) or lies outside [0, rows) are left out; the latter raise status.
- * 0 <= n_ids < 2^31, rows < 2^31, cols <= 2^24.  workspace: atomo_embedding_workspace_bytes (0, and NULL will do, for short lists; -1 on bad arguments).  */
+ * 0 <= n_ids < 2^31, rows < 2^31, cols <= 2^22.  workspace: atomo_embedding_workspace_bytes (0, and NULL will do, for short lists; -1 on bad arguments).  */
 int atomo_embedding(atomo_ctx* ctx, const void* table /*DEVICE*/, int32_t type, int64_t rows, int64_t cols, int64_t ld,
                     const void* ids /*DEVICE*/, int32_t id_bytes, int64_t n_ids, double scale, void* out /*DEVICE*/, int64_t ld_out,
                     int32_t* status /*DEVICE or NULL*/, void* stream);
@@ -332,7 +332,7 @@ int atomo_embedding_backward(atomo_ctx* ctx, const void* ids /*DEVICE*/, int32_t
  * Over the cols values of each row: y = (x - mean) rstd weight + bias, rstd = 1 / sqrt(variance + eps).  x and y are rows x cols of `type` with
  * leading dimensions; weight and bias (either may be NULL: ones, zeros) cols values of weight_type; mean and rstd fp32[rows] are kept for the
  * backward pass, which gives dx (rows x cols of `type`) and, where not NULL, the sums over the rows dweight and dbias (fp32[cols]).
- * y may be x, and dx may be dy or x (same leading dimension).  0 <= rows <= 2^30, 1 <= cols <= 2^24, eps >= 0.
+ * y may be x, and dx may be dy or x (same leading dimension).  0 <= rows <= 2^30, 1 <= cols <= 2^22, eps >= 0.
  * workspace: atomo_layer_norm_workspace_bytes (0, and NULL will do, for a few rows; -1 on bad arguments).                           */
 int atomo_layer_norm(atomo_ctx* ctx, const void* x /*DEVICE*/, int32_t type, int64_t rows, int64_t cols, int64_t ld, const void* weight /*DEVICE or NULL*/,
                      const void* bias /*DEVICE or NULL*/, int32_t weight_type, double eps, void* y /*DEVICE*/, int64_t ld_y, float* mean /*DEVICE*/,

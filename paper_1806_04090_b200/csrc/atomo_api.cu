@@ -370,7 +370,7 @@ bool bad_type(int type) { return type < ATOMO_TYPE_F32 || type > ATOMO_TYPE_F16;
 bool off_type(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
 // null, or not aligned to its elements
 bool bad_ptr(const void* p, int bytes) { return !p || off_type(p, bytes); }
-constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1, kMostCols = (int64_t)1 << 24, kNormRows = (int64_t)1 << 30;
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1, kMostCols = (int64_t)1 << 22, kNormRows = (int64_t)1 << 30;
 // rows x cols with a leading dimension: offsets stay within 62 bits
 bool bad_shape(int64_t rows, int64_t cols, int64_t ld) { return rows < 0 || rows > kMostRows || cols <= 0 || cols > kMostCols || ld < cols || ld > (int64_t)1 << 31; }
 bool bad_tensors(const atomo_tensor* t, int32_t n) {

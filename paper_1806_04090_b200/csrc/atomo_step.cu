@@ -94,6 +94,7 @@ template <int N, bool ONE>
 __global__ void __launch_bounds__(kNormThreads) norm_kernel(const __grid_constant__ NormBatch<N> B) {
   __shared__ double s_warp[kNormThreads / 32];
   __shared__ double s_ctas[kNormCluster];
+  if constexpr (ONE) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");       // this CTA runs: its shared memory may be written to
   const uint32_t per = (B.chunks + gridDim.x - 1) / gridDim.x;
   const uint32_t first = blockIdx.x * per, last = min(first + per, B.chunks);
   double acc = 0.0;
@@ -125,6 +126,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const __grid_constan
   }
   const double sum = block_sum(acc, s_warp);
   if constexpr (ONE) {
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (threadIdx.x == 0) {
       uint32_t remote, local = (uint32_t)__cvta_generic_to_shared(&s_ctas[blockIdx.x]);
       asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(0));
@@ -247,6 +249,11 @@ template <int N> struct AdamBatch {
   int n; AdamHyper h;
 };
 
+// the gradient's factor; false where its norm was not finite: then nothing is updated
+__device__ __forceinline__ bool adam_factor(const AdamHyper& h, float& c) {
+  c = h.scale ? h.scale[1] : 1.0f;
+  return fabsf(c) <= 3.4028235e38f;
+}
 __device__ __forceinline__ float root(float x) { float r; asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
 __device__ __forceinline__ void adam_element(const AdamHyper& h, float c, float decay, float g, float& p, float& m, float& v) {
@@ -420,7 +427,9 @@ __device__ __forceinline__ uint4 pack4(const float (&x)[4], int type) {
 }
 
 template <int BITS>
-__device__ __noinline__ void adam_any(const AdamTensor& t, const AdamHyper& h, int64_t first, float c) {
+__device__ __noinline__ void adam_any(const AdamTensor& t, const AdamHyper& h, int64_t first) {
+  float c;
+  if (!adam_factor(h, c)) return;
   constexpr int kSize = BITS / 8;                                // bytes of a state
   const bool vec = t.vec != 0u, has_master = t.master != nullptr;
   const int psize = type_bytes(t.type);
@@ -497,9 +506,8 @@ template <typename T, int PER> __device__ __forceinline__ void store_group(T* p,
 
 // Elements per group: with 8-bit states eight, so that four lanes share a block.
 template <int BITS, typename P, typename G, bool MASTER>
-__device__ __forceinline__ void adam_inside(const AdamTensor& t, const AdamHyper& h, int64_t first, float c) {
+__device__ __forceinline__ void adam_inside(const AdamTensor& t, const AdamHyper& h, int64_t first) {
   constexpr int PER = BITS == 8 ? 8 : 4, kGroups = kAdamChunk / (kAdamThreads * PER);
-  const AdamPairs k = adam_pairs(h, c, -h.lr * t.decay);
   P* tp = static_cast<P*>(t.p) + first + threadIdx.x * PER;
   float* tw = t.master + first + threadIdx.x * PER;
   const G* tg = static_cast<const G*>(t.g) + first + threadIdx.x * PER;
@@ -516,6 +524,9 @@ __device__ __forceinline__ void adam_inside(const AdamTensor& t, const AdamHyper
       load_group<float, PER>(tm + u * kStep, m[u]);
       load_group<float, PER>(tv + u * kStep, v[u]);
     }
+    float c;
+    if (!adam_factor(h, c)) return;
+    const AdamPairs k = adam_pairs(h, c, -h.lr * t.decay);
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
       constexpr int kStep = kAdamThreads * PER;
@@ -541,6 +552,9 @@ __device__ __forceinline__ void adam_inside(const AdamTensor& t, const AdamHyper
       load_group<G, PER>(tg + u * kStep, g[u]);
       if constexpr (MASTER) load_group<float, PER>(tw + u * kStep, p[u]); else load_group<P, PER>(tp + u * kStep, p[u]);
     }
+    float c;
+    if (!adam_factor(h, c)) return;
+    const AdamPairs k = adam_pairs(h, c, -h.lr * t.decay);
 #pragma unroll
     for (int u = 0; u < kGroups; ++u) {
       constexpr int kStep = kAdamThreads * PER;
@@ -575,25 +589,23 @@ __global__ void __launch_bounds__(kAdamThreads, 5) adamw_kernel(const __grid_con
   const AdamTensor& t = B.t[lo];
   const AdamHyper& h = B.h;
   const int64_t first = (int64_t)(blockIdx.x - B.chunk0[lo]) * kAdamChunk;
-  const float c = h.scale ? h.scale[1] : 1.0f;
-  if (!(fabsf(c) <= 3.0e38f)) return;                             // the gradient's norm was not finite: nothing is updated
   if (t.vec && first + kAdamChunk <= t.n && h.eps >= kEpsPairs) {
     const bool same = h.grad_type == t.type, wide = h.grad_type == ATOMO_TYPE_F32, master = t.master != nullptr;
     if (t.type == ATOMO_TYPE_F32) {
-      if (!master && wide) return adam_inside<BITS, float, float, false>(t, h, first, c);
+      if (!master && wide) return adam_inside<BITS, float, float, false>(t, h, first);
     } else if (t.type == ATOMO_TYPE_BF16) {
-      if (master && wide) return adam_inside<BITS, __nv_bfloat16, float, true>(t, h, first, c);
-      if (master && same) return adam_inside<BITS, __nv_bfloat16, __nv_bfloat16, true>(t, h, first, c);
-      if (!master && wide) return adam_inside<BITS, __nv_bfloat16, float, false>(t, h, first, c);
-      if (!master && same) return adam_inside<BITS, __nv_bfloat16, __nv_bfloat16, false>(t, h, first, c);
+      if (master && wide) return adam_inside<BITS, __nv_bfloat16, float, true>(t, h, first);
+      if (master && same) return adam_inside<BITS, __nv_bfloat16, __nv_bfloat16, true>(t, h, first);
+      if (!master && wide) return adam_inside<BITS, __nv_bfloat16, float, false>(t, h, first);
+      if (!master && same) return adam_inside<BITS, __nv_bfloat16, __nv_bfloat16, false>(t, h, first);
     } else {
-      if (master && wide) return adam_inside<BITS, __half, float, true>(t, h, first, c);
-      if (master && same) return adam_inside<BITS, __half, __half, true>(t, h, first, c);
-      if (!master && wide) return adam_inside<BITS, __half, float, false>(t, h, first, c);
-      if (!master && same) return adam_inside<BITS, __half, __half, false>(t, h, first, c);
+      if (master && wide) return adam_inside<BITS, __half, float, true>(t, h, first);
+      if (master && same) return adam_inside<BITS, __half, __half, true>(t, h, first);
+      if (!master && wide) return adam_inside<BITS, __half, float, false>(t, h, first);
+      if (!master && same) return adam_inside<BITS, __half, __half, false>(t, h, first);
     }
   }
-  adam_any<BITS>(t, h, first, c);
+  adam_any<BITS>(t, h, first);
 }
 
 bool apart(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }

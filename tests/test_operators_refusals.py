@@ -62,7 +62,7 @@ def test_embedding(ctx):
     def look(table=GOOD, kind=0, rows=8, cols=4, ld=4, ids=GOOD, width=8, n=3, scale=1.0, out=GOOD, ld_out=4, status=None):
         return lib.atomo_embedding(h, table, kind, rows, cols, ld, ids, width, n, scale, out, ld_out, status, None)
 
-    for bad in (dict(table=None), dict(table=GOOD + 2), dict(kind=5), dict(rows=0), dict(rows=1 << 31), dict(cols=0), dict(cols=(1 << 24) + 1, ld=1 << 25, ld_out=1 << 25), dict(ld=3),
+    for bad in (dict(table=None), dict(table=GOOD + 2), dict(kind=5), dict(rows=0), dict(rows=1 << 31), dict(cols=0), dict(cols=(1 << 22) + 1, ld=1 << 25, ld_out=1 << 25), dict(ld=3),
                 dict(ids=None), dict(ids=GOOD + 4), dict(width=2), dict(n=-1), dict(n=1 << 31), dict(scale=float("nan")), dict(out=None), dict(ld_out=3), dict(status=GOOD + 1)):
         assert look(**bad) == INVALID, bad
 
@@ -85,7 +85,7 @@ def test_layer_norm(ctx):
     def forward(x=GOOD, kind=0, rows=3, cols=4, ld=4, w=GOOD, b=GOOD, wkind=0, eps=1e-5, y=GOOD, ld_y=4, mean=GOOD, rstd=GOOD):
         return lib.atomo_layer_norm(h, x, kind, rows, cols, ld, w, b, wkind, eps, y, ld_y, mean, rstd, None)
 
-    for bad in (dict(x=None), dict(x=GOOD + 2), dict(kind=3), dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(cols=(1 << 24) + 1, ld=1 << 25, ld_y=1 << 25), dict(ld=3), dict(w=GOOD + 2),
+    for bad in (dict(x=None), dict(x=GOOD + 2), dict(kind=3), dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(cols=(1 << 22) + 1, ld=1 << 25, ld_y=1 << 25), dict(ld=3), dict(w=GOOD + 2),
                 dict(b=GOOD + 1), dict(wkind=7), dict(eps=-1.0), dict(eps=float("nan")), dict(y=None), dict(ld_y=3), dict(mean=None), dict(rstd=None)):
         assert forward(**bad) == INVALID, bad
 
