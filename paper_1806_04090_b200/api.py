@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 import os
 import struct
 from dataclasses import dataclass, field
@@ -215,6 +216,7 @@ def measure_fma_peak(device: int = 0, fp64: bool = False) -> float:
 
 
 _ADAMW_ARGS = struct.Struct("=ddddqQQii").pack          # _AdamWArgs
+_T, _dtype_of = torch.Tensor, operator.attrgetter("dtype")
 
 
 def default_k_cap(s: float, n_atoms: int) -> int:
@@ -673,20 +675,28 @@ class Atomo:
         that clips them (NaN where the norm is not finite), as atomo_adamw takes them.  Gradients: contiguous fp32, bf16 or fp16."""
         if stream is not None:
             return self._on(stream, self.atomo_grad_norm, grads, max_norm, out)
-        device, codes = self.device, TYPE_CODES
-        desc = []                                        # of _Tensor
-        for g in grads:
-            code = codes.get(g.dtype)
-            if code is None or g.get_device() != device or not g.is_contiguous():
-                raise ValueError(f"gradients must be contiguous fp32, bf16 or fp16 tensors on CUDA device {device}")
-            desc += (g.data_ptr(), g.numel(), code)
-        n = len(desc) // 3
+        device, n = self.device, len(grads)
+        desc = []                                        # of _Tensor; the type's high half is the reserved word
+        if n <= 4:
+            for g in grads:
+                desc += (g.data_ptr(), g.numel(), TYPE_CODES.get(g.dtype))
+                if desc[-1] is None or g.get_device() != device or not g.is_contiguous():
+                    desc = None
+                    break
+        else:                                            # (of a method mapped over a long list a call takes two thirds of one in a loop)
+            codes = [TYPE_CODES.get(k) for k in map(_dtype_of, grads)]
+            desc = [0] * (3 * n)
+            desc[0::3], desc[1::3], desc[2::3] = map(_T.data_ptr, grads), map(_T.numel, grads), codes
+            if None in codes or not all(map(_T.is_contiguous, grads)) or any(map(device.__ne__, map(_T.get_device, grads))):
+                desc = None
+        if desc is None:
+            raise ValueError(f"gradients must be contiguous fp32, bf16 or fp16 tensors on CUDA device {device}")
         if out is None:
             out = self._floats.new_empty(2)
         elif not (out.get_device() == device and out.dtype == torch.float32 and out.numel() == 2 and out.is_contiguous()):
             raise ValueError(f"out: two fp32 numbers on CUDA device {device} are required")
         s = self._own_stream()
-        packed = struct.pack("=" + "qqq" * n, *desc)     # (the type's high half is the reserved word)
+        packed = struct.pack("=%dq" % (3 * n), *desc)
         nbytes = self.lib.atomo_grad_norm_workspace_bytes(packed, n)
         if nbytes < 0:
             raise AtomoError(1, "atomo_grad_norm_workspace_bytes")
@@ -707,17 +717,13 @@ class Atomo:
         if state.device.index != device:
             raise ValueError(f"the parameters are on {state.device}, the context on device {device}")
         kind = grads[0].dtype
-        if kind not in TYPE_CODES:
-            raise ValueError("gradients must be fp32, bf16 or fp16")
-        ptrs = []
-        for g, size in zip(grads, state.lengths):
-            if g.dtype is not kind or g.numel() != size or g.get_device() != device or not g.is_contiguous():
-                raise ValueError(f"gradients must be contiguous tensors of one type on CUDA device {device}, with as many elements as their parameters")
-            ptrs.append(g.data_ptr())
+        if not (kind in TYPE_CODES and set(map(_dtype_of, grads)) == {kind} and set(map(_T.get_device, grads)) == {device} and list(map(_T.numel, grads)) == state.lengths
+                and all(map(_T.is_contiguous, grads))):
+            raise ValueError(f"gradients must be contiguous tensors on CUDA device {device}, of one type (fp32, bf16 or fp16), with as many elements as their parameters")
         if scale is not None and not (scale.get_device() == device and scale.dtype == torch.float32 and scale.numel() == 2 and scale.is_contiguous()):
             raise ValueError(f"scale: two fp32 numbers on CUDA device {device} are required")
         args = _ADAMW_ARGS(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, 0 if scale is None else scale.data_ptr(), state.bits, TYPE_CODES[kind])
-        rc = self.lib.atomo_adamw(self._h, state._desc, struct.pack("=%dQ" % n, *ptrs), n, args, self._own_stream())
+        rc = self.lib.atomo_adamw(self._h, state._desc, struct.pack("=%dQ" % n, *map(_T.data_ptr, grads)), n, args, self._own_stream())
         self._check(rc, "atomo_adamw")
 
     def _status(self, status: Optional[torch.Tensor]):

@@ -11,7 +11,8 @@
 //   emb_sum_kernel    chunks of kEmbChunk neighbouring sorted tokens, so that a frequent token's run is split among CTAs.  A run that ends in the chunk it
 //                     starts in, or in the next one, is summed by the former and goes to its row; a longer one leaves one part per chunk in the workspace.
 //   emb_join_kernel   adds the parts of the longer runs, in order.
-// What bounds it is memory: dout is read once, the table's gradient written once.
+// What bounds it is memory: dout is read once, the table's gradient written once.  64k tokens of 2048 bf16 columns, 32000 rows, 530 MB in all: sort 25 us beside
+// the zero rows' 39, sums 64 (6.1 TB/s), join 14.
 // Short lists go through emb_direct_kernel, which does all of it: a CTA has every so-manieth row of the table (frequent ids often lie side by side) and some
 // columns, finds the tokens of its rows among all ids, sorts them in shared memory and sums them; and it has a stretch of rows in which it writes those without
 // tokens.  A launch instead of three, and no wait between them.
@@ -50,26 +51,43 @@ EmbShape emb_shape(int64_t cols, int vec) {
 
 // ---- lookup ---------------------------------------------------------------------------------------
 // A CTA goes on to other tokens, whose ids it fetches while the rows are under way; what it writes is not kept in L2 for long, so that the rows of frequent
-// tokens stay.  64k tokens of 2048 bf16, us, CTAs per SM x tokens at a time: 6 x 2 60, 5 x 2 62, 6 x 1 64, 4 x 3 66, 4 x 4 66, 4 x 2 68, 3 x 4 70, 7 x 2 and
-// 8 x 2 (spills) 72; one CTA per two tokens, many more than fit: 84; without the streaming stores 72 at best.
-constexpr int kLookCtas = 6, kLookTokens = 2;
+// tokens stay.  64k tokens of 2048 bf16, us, CTAs per SM x tokens at a time: 5 x 2 57, 6 x 2 59 (the order of 4 x 2, 4 x 3, 3 x 4, 8 x 2 behind them: 64 to 72); one
+// CTA per two tokens, many more than fit: 84; without the streaming stores 72 at best.
+// A thread has one pack of 16 bytes of a row, or four smaller ones (what a token costs it, 60 instructions, is shared by them).
+constexpr int kLookCtas = 5, kLookTokens = 2;
+template <typename T, int VEC> __host__ __device__ constexpr int look_packs() { return VEC * sizeof(T) == 16 ? 1 : 4; }
+template <typename T, int VEC>
+__device__ __forceinline__ void scale_pack(Pack<T, VEC>& x, float scale) {
+  if constexpr (VEC > 1) {
+    const uint64_t both = pack2(scale, scale);
+#pragma unroll
+    for (int j = 0; j < VEC; j += 2) pair_to(x.v + j, mul2(pair_of(x.v + j), both));
+  } else x.v[0] = from_float<T>(to_float(x.v[0]) * scale);
+}
 template <typename T, int VEC, int U>
 __global__ void __launch_bounds__(kEmbThreads, kLookCtas) emb_lookup_kernel(const T* __restrict__ table, int64_t rows, int64_t cols, int64_t ld, Ids ids, int64_t n,
                                                                  float scale, T* __restrict__ out, int64_t ld_out, int32_t* status) {
-  const int64_t col = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC, step = (int64_t)gridDim.x * U * blockDim.y;
+  constexpr int P = look_packs<T, VEC>();
+  const int64_t col = ((int64_t)blockIdx.y * P * blockDim.x + threadIdx.x) * VEC, step = (int64_t)gridDim.x * U * blockDim.y;
+  const int hop = blockDim.x * VEC;                              // between a thread's packs
   if (col >= cols) return;
   int64_t id[U], t0 = (int64_t)blockIdx.x * U * blockDim.y + threadIdx.y;
 #pragma unroll
   for (int u = 0; u < U; ++u) { const int64_t t = t0 + (int64_t)u * blockDim.y; id[u] = t < n ? load_id(ids, t) : -1; }
   for (; t0 < n; t0 += step) {
-    Pack<T, VEC> x[U];
+    Pack<T, VEC> x[U][P];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (id[u] >= 0 && id[u] < rows) x[u] = load_pack<T, VEC>(table + id[u] * ld + col);
-      else {
-        if (col == 0 && t0 + (int64_t)u * blockDim.y < n) raise_word(status);
+      const bool valid = id[u] >= 0 && id[u] < rows;
+      if (!valid && col == 0 && t0 + (int64_t)u * blockDim.y < n) raise_word(status);
+      const T* from = table + id[u] * ld + col;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) x[u].v[j] = from_float<T>(0.0f);
+      for (int p = 0; p < P; ++p) {
+        if (valid && col + p * hop < cols) x[u][p] = load_pack<T, VEC>(from + p * hop);
+        else {
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) x[u][p].v[j] = from_float<T>(0.0f);
+        }
       }
     }
 #pragma unroll
@@ -78,10 +96,15 @@ __global__ void __launch_bounds__(kEmbThreads, kLookCtas) emb_lookup_kernel(cons
     for (int u = 0; u < U; ++u) {
       const int64_t t = t0 + (int64_t)u * blockDim.y;
       if (t < n) {
+        T* to = out + t * ld_out + col;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) x[u].v[j] = from_float<T>(to_float(x[u].v[j]) * scale);
-        if constexpr (VEC * sizeof(T) == 16) __stcs(reinterpret_cast<uint4*>(out + t * ld_out + col), *reinterpret_cast<uint4*>(&x[u]));
-        else store_pack<T, VEC>(out + t * ld_out + col, x[u]);
+        for (int p = 0; p < P; ++p) {
+          if (col + p * hop < cols) {
+            scale_pack(x[u][p], scale);
+            if constexpr (VEC * sizeof(T) == 16) __stcs(reinterpret_cast<uint4*>(to), *reinterpret_cast<uint4*>(&x[u][p]));
+            else store_pack<T, VEC>(to + p * hop, x[u][p]);
+          }
+        }
       }
     }
   }
@@ -623,6 +646,7 @@ __global__ void __launch_bounds__(kDirectThreads, 2) emb_direct_kernel(const __g
     }
     flush(part ? 0 : end < count && (int)(s_keys[end] >> kDirectBits) == run ? 1 : -1);
   }
+  // (last: before the sums, whose loads then wait behind these stores, the whole took a tenth longer)
   for (int r = warp; r < rows; r += kDirectWarps) if (!s_seen[r]) zero_row(a.out + (z0 + r) * a.ld_out, a.cols, a.vec_out);
   // the runs that went over: their parts in order, a thread per column
   __syncthreads();
@@ -649,7 +673,7 @@ int emb_vec(const void* base, int64_t ld, int64_t cols, int size) {
 
 template <typename T, int VEC>
 cudaError_t lookup_typed(const EmbLookup& a, cudaStream_t st) {
-  const EmbShape s = emb_shape(a.cols, VEC);
+  const EmbShape s = emb_shape(a.cols, VEC * look_packs<T, VEC>());
   const dim3 block(s.cx, s.cy);
   // several tokens at a time from where so many fewer threads still fill the GPU
   const bool many = a.n * s.slabs * s.cx / kLookTokens >= 148 * 2048;

@@ -371,8 +371,9 @@ def test_refused_tensors(atomo):
             atomo.atomo_adamw(state, [g], **args)
         assert e.value.code == 1
     for bad in (g.cpu(), g.double(), torch.zeros(128, device="cuda")[::2]):
-        with pytest.raises(ValueError):
-            atomo.atomo_grad_norm([bad])
+        for others in (0, 3, 10):
+            with pytest.raises(ValueError):
+                atomo.atomo_grad_norm([g] * others + [bad] + [g] * others)
     with pytest.raises(api.AtomoError):
         atomo.atomo_grad_norm([])
     with pytest.raises(api.AtomoError):
