@@ -272,7 +272,7 @@ typedef struct { const void* data; /* DEVICE */ int64_t n; int32_t type; /* atom
  * out[0] = sqrt(sum of the squares of all elements of all tensors), out[1] = min(1, max_norm / (out[0] + 1e-6)): the norm and the
  * factor that clips the gradients to it.  max_norm > 0; INFINITY asks for the norm alone (factor 1).  The sum neither
  * overflows nor underflows: out[0] is the norm rounded to fp32.  Where an element is NaN or Inf the norm is not finite and
- * the factor is NaN.  Tensors may be empty; at most 2^20 of them.  workspace: atomo_grad_norm_workspace_bytes (0, and NULL will do, where little is
+ * the factor is NaN.  Tensors may be empty; at most 2^20 of them, of 2^40 values in all.  workspace: atomo_grad_norm_workspace_bytes (0, and NULL will do, where little is
  * to be read; -1 on bad arguments).                                                                                              */
 int64_t atomo_grad_norm_workspace_bytes(const atomo_tensor* grads /*HOST array*/, int32_t n_tensors);
 int atomo_grad_norm(atomo_ctx* ctx, const atomo_tensor* grads /*HOST array*/, int32_t n_tensors, double max_norm,
@@ -291,7 +291,7 @@ int atomo_grad_norm(atomo_ctx* ctx, const atomo_tensor* grads /*HOST array*/, in
  * average would stand still where a step changes it by less than half a unit), by the Philox words of the conventions
  * above with key = seed and counter = (i>>2 low, 2^31 | i>>2 high, tensor, step & 0x7fffffff), which no encode uses: element i takes the low 16 bits of
  * word i&3 for the first moment, the high ones for the second.  A second moment above zero is not rounded to zero.  A state that is not finite becomes NaN.
- * The parameters in `tensors` and their states do not overlap; a parameter may be empty.  Every n < 2^34 with 8-bit states.      */
+ * Parameters, states and gradients do not overlap; a parameter may be empty.  Every n < 2^34 with 8-bit states.      */
 enum { ATOMO_STATE_BLOCK = 32 };
 typedef struct {
   void* param;                                  /* DEVICE, type                                 */
@@ -314,7 +314,7 @@ int atomo_adamw(atomo_ctx* ctx, const atomo_adamw_tensor* tensors /*HOST array*/
 
 /* --- embedding -----------------------------------------------------------------------------------
  * out[t] = scale * table[ids[t]]: table is rows x cols of `type` with leading dimension ld, out n_ids x cols of the same type with
- * leading dimension ld_out; ids are 4 or 8 bytes wide (id_bytes).  An id outside [0, rows) gives a row of zeros and, where status (DEVICE,
+ * leading dimension ld_out and does not overlap it; ids are 4 or 8 bytes wide (id_bytes).  An id outside [0, rows) gives a row of zeros and, where status (DEVICE,
  * one int32, set to 0 by the caller) is not NULL, ATOMO_ERR_INVALID_ARG in it.
  * Backward: out[v] = scale * sum of grad[t] over the tokens t with ids[t] = v, in the order of the tokens; out is fp32, every
  * element of its rows x cols is written (accumulate != 0: added to what is there).  grad is n_ids x cols of `type`, leading dimension ld.  Tokens whose id
@@ -332,7 +332,7 @@ int atomo_embedding_backward(atomo_ctx* ctx, const void* ids /*DEVICE*/, int32_t
  * Over the cols values of each row: y = (x - mean) rstd weight + bias, rstd = 1 / sqrt(variance + eps).  x and y are rows x cols of `type` with
  * leading dimensions; weight and bias (either may be NULL: ones, zeros) cols values of weight_type; mean and rstd fp32[rows] are kept for the
  * backward pass, which gives dx (rows x cols of `type`) and, where not NULL, the sums over the rows dweight and dbias (fp32[cols]).
- * y may be x, and dx may be dy or x (same leading dimension).  0 <= rows <= 2^30, 1 <= cols <= 2^22, eps >= 0.
+ * y may be x, and dx may be dy or x (same leading dimension).  A row's variance has to lie in the range of fp32.  0 <= rows <= 2^30, 1 <= cols <= 2^22, eps >= 0.
  * workspace: atomo_layer_norm_workspace_bytes (0, and NULL will do, for a few rows; -1 on bad arguments).                           */
 int atomo_layer_norm(atomo_ctx* ctx, const void* x /*DEVICE*/, int32_t type, int64_t rows, int64_t cols, int64_t ld, const void* weight /*DEVICE or NULL*/,
                      const void* bias /*DEVICE or NULL*/, int32_t weight_type, double eps, void* y /*DEVICE*/, int64_t ld_y, float* mean /*DEVICE*/,

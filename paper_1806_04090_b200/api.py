@@ -351,7 +351,7 @@ def _rows(t: torch.Tensor, cols: int, what: str):
     if len(shape) == 0 or shape[-1] != cols or (cols > 1 and stride[-1] != 1):
         raise ValueError(f"{what}: a tensor with {cols} values in its last dimension, of unit stride, is required")
     if t.is_contiguous():
-        return t.numel() // cols, cols
+        return t.numel() // max(cols, 1), cols
     if len(shape) == 1:
         return 1, cols
     rows, ld = shape[-2], stride[-2] if shape[-2] > 1 else cols

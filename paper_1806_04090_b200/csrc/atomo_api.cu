@@ -375,8 +375,12 @@ constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1, kMostCols = (int64_t)1 << 
 bool bad_shape(int64_t rows, int64_t cols, int64_t ld) { return rows < 0 || rows > kMostRows || cols <= 0 || cols > kMostCols || ld < cols || ld > (int64_t)1 << 31; }
 bool bad_tensors(const atomo_tensor* t, int32_t n) {
   if (!t || n <= 0 || n > 1 << 20) return true;
-  for (int i = 0; i < n; ++i) if (t[i].n < 0 || t[i].n > (int64_t)1 << 40 || bad_type(t[i].type)) return true;
-  return false;
+  int64_t all = 0;                   // in all 2^40 values at most: the chunks of a launch are counted in 32 bits
+  for (int i = 0; i < n; ++i) {
+    if (t[i].n < 0 || t[i].n > (int64_t)1 << 40 || bad_type(t[i].type)) return true;
+    all += t[i].n;
+  }
+  return all > (int64_t)1 << 40;
 }
 // runs f on the context's device; nothing is thrown through the C boundary
 template <typename F> int on_device(atomo_ctx* ctx, const char* what, F f) {

@@ -15,7 +15,7 @@
 // the zero rows' 39, sums 64 (6.1 TB/s), join 14.
 // Short lists go through emb_direct_kernel, which does all of it: a CTA has every so-manieth row of the table (frequent ids often lie side by side) and some
 // columns, finds the tokens of its rows among all ids, sorts them in shared memory and sums them; and it has a stretch of rows in which it writes those without
-// tokens.  A launch instead of three, and no wait between them.
+// tokens.  A launch instead of four, and no wait between them.
 #include <algorithm>
 
 #include "atomo_ops.cuh"
@@ -520,7 +520,7 @@ template <typename T, int VEC> struct DirectShape {              // columns of a
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kDirectThreads, 2) emb_direct_kernel(const __grid_constant__ DirectArgs a) {
   constexpr int PACKS = DirectShape<T, VEC>::kPacks, COLS = DirectShape<T, VEC>::kCols, kAhead = VEC * sizeof(T) == 16 && sizeof(T) == 2 ? 4 : 8;
-  extern __shared__ uint32_t s_keys[];                           // [padded] row << 13 | token; then [2][warps][COLS] parts of runs, a flag per row
+  extern __shared__ uint32_t s_keys[];                           // [padded] row << kDirectBits | token; then [2][warps][COLS] parts of runs, a flag per row
   float* s_part = reinterpret_cast<float*>(s_keys + a.padded);
   uint8_t* s_seen = reinterpret_cast<uint8_t*>(s_part + 2 * kDirectWarps * COLS);
   __shared__ int s_count, s_row[2][kDirectWarps + 1];            // rows of the parts, -1: none
@@ -793,15 +793,16 @@ int launch_embedding(const EmbLookup& a, cudaStream_t st) {
   return (int)lookup_type<__half>(a, st);
 }
 
-uint64_t embedding_workspace(int64_t n, int64_t cols) { return n <= kDirectMost ? 0 : emb_layout(n, cols).bytes; }
+// One launch, or four.  Kernels alone, us, one | four (tokens x rows x columns, fp32): 256 x 21294 x 38 6 | 19, 1000 x 5000 x 64 6 | 24, 1000 x 32000 x 1024 27 | 34,
+// 2000 x 32000 x 2048 56 | 57, 3000 x 32000 x 1024 36 | 36, 4000 x 16000 x 1024 28 | 27, 4000 x 50000 x 512 32 | 30, 4001 x 10007 x 515 22 | 25, 4000 x 32000 x 2048
+// 66 | 59 (bf16 alike): a frequent id's tokens wait for one CTA, the longer the more there are and the wider they are.
+static bool one_launch(int64_t n, int64_t cols) { return n <= 2048 || (n <= kDirectMost && n * cols <= 5 << 19); }
+uint64_t embedding_workspace(int64_t n, int64_t cols) { return one_launch(n, cols) ? 0 : emb_layout(n, cols).bytes; }
 
 int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
   if (b.n == 0 && b.accumulate) return (int)cudaSuccess;
   const int vec_out = reinterpret_cast<uintptr_t>(b.out) % 16 == 0 && b.ld_out % 4 == 0;
-  // One launch, or three.  Kernels alone, us, one | three (tokens x rows x columns, fp32): 1 x 50000 x 64 7 | 13, 256 x 21294 x 38 6 | 18,
-  // 1000 x 5000 x 64 6 | 22, 1000 x 32000 x 1024 27 | 32, 4001 x 10007 x 515 22 | 24, 4000 x 10000 x 512 21 | 22, 4000 x 32000 x 2048 59 | 60; longer lists, where
-  // a frequent id's tokens wait for one CTA: 8000 x 32000 x 512 42 | 26.
-  if (b.n <= kDirectMost) {
+  if (one_launch(b.n, b.cols)) {
     DirectArgs d{};
     d.ids = Ids{b.ids, b.id_bytes == 8}; d.n = (int)b.n; d.rows = b.rows; d.cols = b.cols; d.padding = b.padding; d.dout = b.grad; d.ld = b.ld;
     d.scale = b.scale; d.accumulate = b.accumulate; d.out = b.out; d.ld_out = b.ld_out; d.vec_out = vec_out; d.status = b.status;

@@ -15,6 +15,7 @@
 // one exchange and loses nothing where the mean is far from zero.  All arithmetic is in fp32; y and dx are rounded to their type once.
 // Rows of more than kNormCols columns do not fit: CTAs then read them again from L2.
 #include <algorithm>
+#include <atomic>
 
 #include "atomo_ops.cuh"
 
@@ -563,12 +564,13 @@ template <typename T, typename F> cudaError_t by_form(int bytes, int64_t cols, F
 }
 // CTAs of a kernel that the GPU holds at a time.  What its registers allow is asked for once per number of warps (`known`: 0 before that); then what shared
 // memory does, 227 KB of it with 1 KB for each CTA and what it has besides the ring.
-int resident(const void* kernel, int threads, size_t smem, int (&known)[17]) {
-  int& n = known[threads / 32];
+int resident(const void* kernel, int threads, size_t smem, std::atomic<int> (&known)[17]) {
+  int n = known[threads / 32].load(std::memory_order_relaxed);
   if (n == 0) {
     int per = 0;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, kernel, threads, 0) != cudaSuccess) cudaGetLastError();
     n = std::max(per, 1);
+    known[threads / 32].store(n, std::memory_order_relaxed);
   }
   return 148 * std::max(1, std::min(n, (int)(227 * 1024 / (smem + 2048))));
 }
@@ -585,7 +587,7 @@ cudaError_t forward_cta(const NormForward& a, Shape s, cudaStream_t st) {
   constexpr int R = rows_per_step(VEC * PACKS * (int)sizeof(T));
   const int64_t step = (int64_t)s.threads / s.width * R;         // rows of a CTA's step
   const size_t smem = Ring<T, VEC, PACKS, R, kForwardStages, CTA>::bytes(s.threads / s.width, (int)a.cols);
-  static int known[17];
+  static std::atomic<int> known[17];
   const int grid = (int)std::min<int64_t>((a.rows + step - 1) / step, resident((const void*)ln_forward_kernel<T, VEC, PACKS, CTA>, s.threads, smem, known));
   ln_forward_kernel<T, VEC, PACKS, CTA><<<grid, s.threads, smem, st>>>(s.width, (const T*)a.x, a.rows, (int)a.cols, a.ld, Weight{a.weight, a.weight_type}, Weight{a.bias, a.weight_type}, a.eps,
                                                                        (T*)a.y, a.ld_y, a.mean, a.rstd);
@@ -621,7 +623,7 @@ cudaError_t backward_cta(const NormBackward& a, Shape s, cudaStream_t st) {
   constexpr int R = rows_per_step(VEC * PACKS * (int)sizeof(T));
   const int beside = s.threads / s.width;
   const size_t smem = std::max<size_t>(Ring<T, VEC, PACKS, 2 * R, kBackwardStages, CTA>::bytes(beside, (int)a.cols), beside > 1 ? (size_t)beside * 2 * a.cols * 4 : 0);
-  static int known[17];
+  static std::atomic<int> known[17];
   // a few steps: one CTA, whose sums are the results (the join is a launch, and 3 us)
   const bool one = a.rows <= 4 * beside * R;
   const int grid = one ? 1 : std::min(back_ctas(a.rows, (int64_t)beside * R), resident((const void*)ln_backward_kernel<T, VEC, PACKS, CTA>, s.threads, smem, known));

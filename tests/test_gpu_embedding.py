@@ -104,7 +104,7 @@ def test_gradient_lengths(atomo, kind, n):
 
 @pytest.mark.parametrize("rows", [1, 2, 255, 256, 65535, 65536, 70001])
 def test_gradient_table_sizes(atomo, rows):
-    """Keys of one to three passes, among them the largest of a number of bits."""
+    """Among them the largest numbers of a number of bits."""
     gen = _gen(4)
     ids = _ids("random", 3000, rows, gen)
     ids[::7] = rows - 1
@@ -174,6 +174,31 @@ def test_gradient_repeats_bit_for_bit(atomo):
     for _ in range(10):
         torch.empty(1 << 24, dtype=torch.uint8, device="cuda").random_()      # other work of the allocator in between
         assert torch.equal(atomo.atomo_embedding_backward(ids, grad, 500), first)
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("rows,cols,n", [(255, 130, 5000), (256, 8, 4097), (65535, 3, 8193), (70001, 12, 6000), (1, 33, 4500), ((1 << 24) + 5, 1, 5001), (900, 1025, 2600),
+                                         (300, 2048, 2049), (900, 7, 131073), (65536, 2, 150001), ((1 << 24) + 5, 1, 140000), (17, 4104, 4200)])
+def test_gradient_of_long_lists(atomo, rows, cols, n, dtype):
+    """Lists that are sorted by a kernel of their own: keys of one to four passes, several tiles per CTA, ids that are not 16 bytes aligned, padding, ids without a row."""
+    gen = _gen(11)
+    ids = torch.cat([torch.randint(0, rows, (n // 2,), generator=gen, device="cuda"), torch.randint(0, min(rows, 5), (n - n // 2,), generator=gen, device="cuda") * (rows // 5)])
+    ids = ids.clamp(max=rows - 1)[torch.randperm(n, generator=gen, device="cuda")]
+    ids[n // 3], ids[n // 2], ids[-1] = rows, -1, rows - 1
+    padding = rows // 5 if rows > 1 else -1
+    grad = torch.randn(n, cols, generator=gen, device="cuda").to(dtype)
+    want, off = _want(ids, grad, rows, 1.5, padding)
+    for shifted in (torch.empty(n + 1, dtype=torch.int64, device="cuda")[1:], torch.empty(n + 1, dtype=torch.int32, device="cuda")[1:]):
+        shifted.copy_(ids)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        got = atomo.atomo_embedding_backward(shifted, grad, rows, scale=1.5, padding_idx=padding, status=status)
+        ref.near(got, want, off)
+        assert int(status) == 1
+    room = torch.full((rows, cols + 3), 0.25, device="cuda")
+    atomo.atomo_embedding_backward(ids, grad, rows, scale=1.5, padding_idx=padding, out=room[:, 1:cols + 1], accumulate=True)
+    ref.near(room[:, 1:cols + 1], want + 0.25, off + 2 * ref.U32 * (np.abs(want) + 0.25))
+    room[:, 1:cols + 1] = 0.25
+    assert bool((room == 0.25).all())
 
 
 def test_gradient_is_the_lookups_derivative(atomo):

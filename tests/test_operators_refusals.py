@@ -37,6 +37,9 @@ def test_grad_norm(ctx):
                 dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(out=None), dict(out=GOOD + 2), dict(ws=None), dict(ws=GOOD + 4)):
         assert call(**bad) == INVALID, bad
     assert call(size=need - 1) == CAPACITY
+    many = lambda n: (api._Tensor * 2)((GOOD, n, 0, 0), (GOOD, n, 0, 0))              # 2^40 values in all, at most
+    assert size(many(1 << 39), 2) > 0 and size(many((1 << 39) + 1), 2) == -1
+    assert lib.atomo_grad_norm(h, many((1 << 39) + 1), 2, 1.0, GOOD, GOOD, 1 << 20, None) == INVALID
     assert lib.atomo_grad_norm(None, (api._Tensor * 1)((GOOD, 4, 0, 0)), 1, 1.0, GOOD, GOOD, need, None) == INVALID
 
 
