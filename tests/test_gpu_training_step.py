@@ -87,3 +87,41 @@ def test_a_sparse_table_gradient_keeps_its_zero_rows_through_the_exchange(atomo)
         pay, _ = atomo.atomo_encode_entrywise([grad.view(-1)], s, seed=3, step=2)
         out = atomo.atomo_decode(pay)[0].view(ROWS, COLS)
         assert atomo.payload_status(pay)[0] == 0 and bool((out[grad == 0] == 0).all()) and int((out != 0).sum()) > 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("rows,cols,tokens,dtype", [(ROWS, COLS, TOKENS, torch.float32), (700, 520, 6000, torch.bfloat16), (90, 33, 2500, torch.float16)])
+def test_step_as_a_captured_graph(atomo, rows, cols, tokens, dtype, bits):
+    """Forward, backward and update of one worker in one graph: replayed on two batches, bit for bit what the calls give one by one."""
+    from paper_1806_04090_b200 import api
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(33)
+    start = [torch.randn(rows, cols, generator=gen, device="cuda").to(dtype), torch.ones(cols, device="cuda").to(dtype), torch.zeros(cols, device="cuda").to(dtype)]
+    batches = [(torch.randint(0, rows, (tokens,), generator=gen, device="cuda"), torch.randn(tokens, cols, generator=gen, device="cuda").to(dtype)) for _ in range(2)]
+
+    def step(params, state, ids, dy):
+        x = atomo.atomo_embedding(params[0], ids, scale=0.5)
+        y, mean, rstd = atomo.atomo_layer_norm(x, params[1], params[2])
+        dx, dweight, dbias = atomo.atomo_layer_norm_backward(dy, x, params[1], mean, rstd)
+        grads = [atomo.atomo_embedding_backward(ids, dx, rows, scale=0.5), dweight, dbias]
+        atomo.atomo_adamw(state, grads, lr=1e-2, step=3, seed=4, scale=atomo.atomo_grad_norm(grads, max_norm=1.0))
+
+    def run():
+        params = [p.clone() for p in start]
+        return params, api.AdamWState.zeros(params, bits=bits, master=dtype != torch.float32)
+
+    eager, eager_state = run()
+    for ids, dy in batches:
+        step(eager, eager_state, ids, dy)
+    params, state = run()
+    ids, dy = batches[0][0].clone(), batches[0][1].clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(params, state, ids, dy)
+    for batch in batches:
+        ids.copy_(batch[0]); dy.copy_(batch[1])
+        graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(eager + eager_state.exp_avg + eager_state.exp_avg_sq, params + state.exp_avg + state.exp_avg_sq):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
