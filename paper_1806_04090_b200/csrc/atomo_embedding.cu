@@ -369,40 +369,54 @@ __device__ __forceinline__ void put_row(const SumArgs& a, float* p, const float 
   }
 }
 
-// A thread's packs of the gradient's rows on their way: kAhead of them, each thread's own, so that it waits for nobody else's.
-// 16- and 4-byte packs are copied to shared memory asynchronously, which takes no registers; 2-byte ones are loaded.
+// A thread's packs of the gradient's rows on their way: AHEAD rows, each thread's own, so that it waits for nobody else's.  They are copied to shared memory
+// asynchronously, which takes no registers; a 16-bit value with the whole word that it lies in.
+// (Sums of 30000 tokens of 1023 bf16 columns, us: one value per thread, loaded and stored, 103; four values per thread, copied in their words, 55.  10033 tokens of
+// 1155 fp32 columns: 27 and 20.)
 template <typename T, int VEC, int AHEAD>
 struct RowQueue {
-  static constexpr int kBytes = VEC * (int)sizeof(T);
-  static constexpr bool kAsync = kBytes == 16 || kBytes == 4;
-  Pack<T, VEC>* slot; int stride;      // of this thread; packs between two of its slots
-  __device__ __forceinline__ void put(int i, const T* p) {
-    Pack<T, VEC>* s = slot + (i % AHEAD) * stride;
-    if constexpr (kAsync) copy_async<kBytes>(s, p);
-    else *s = load_pack<T, VEC>(p);
+  static constexpr int kBytes = VEC * (int)sizeof(T), kCell = kBytes < 4 ? 4 : kBytes;
+  static constexpr int kPacks = look_packs<T, VEC>(), kPitch = kEmbThreads * kCell;    // of a thread; bytes between two of its cells
+  static constexpr size_t kSize = (size_t)AHEAD * kPacks * kPitch;
+  uint8_t* slot;
+  __device__ __forceinline__ uint8_t* cell(int turn, int k) const { return slot + turn * (kPacks * kPitch) + k * kPitch; }
+  // edge: the word may lie outside the matrix
+  __device__ __forceinline__ void put(int turn, int k, const T* p, bool edge) {
+    if constexpr (kBytes >= 4) copy_async<kBytes>(cell(turn, k), p);
+    else {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+      if (edge) *reinterpret_cast<T*>(cell(turn, k) + (at & 2)) = *p;
+      else copy_async<4>(cell(turn, k), reinterpret_cast<const void*>(at & ~(uintptr_t)3));
+    }
   }
-  __device__ __forceinline__ void close() { if constexpr (kAsync) asm volatile("cp.async.commit_group;" ::: "memory"); }
-  __device__ __forceinline__ Pack<T, VEC> get(int i) {
-    if constexpr (kAsync) asm volatile("cp.async.wait_group %0;" :: "n"(AHEAD - 1) : "memory");
-    return slot[(i % AHEAD) * stride];
+  __device__ __forceinline__ void close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+  __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" :: "n"(AHEAD - 1) : "memory"); }
+  // low: of the pack's address in global memory
+  __device__ __forceinline__ Pack<T, VEC> get(int turn, int k, uint32_t low) const {
+    return *reinterpret_cast<const Pack<T, VEC>*>(cell(turn, k) + (kBytes < 4 ? low & 2u : 0u));
   }
 };
 
 constexpr int kEmbAhead = 12, kWindow = 3 * kEmbChunk + 2;
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kEmbThreads, 4) emb_sum_kernel(const __grid_constant__ SumArgs a) {
-  extern __shared__ uint4 s_raw[];     // [kEmbAhead][threads] packs, then [cy][kWindow] items
+  extern __shared__ uint4 s_raw[];     // [kEmbAhead][threads] packs or words, then [cy][kWindow] items
   wait_for_previous();
   const int tid = threadIdx.y * blockDim.x + threadIdx.x, threads = blockDim.x * blockDim.y;
-  const int64_t col = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * VEC;
-  uint64_t* s_items = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_raw) + (size_t)kEmbAhead * threads * VEC * sizeof(T));
+  using Queue = RowQueue<T, VEC, kEmbAhead>;
+  constexpr int P = Queue::kPacks;
+  const int col = (blockIdx.y * P * blockDim.x + threadIdx.x) * VEC, hop = blockDim.x * VEC, cols = (int)a.cols;       // hop: between a thread's packs
+  bool in[P];                                                    // the packs that lie inside the row
+#pragma unroll
+  for (int k = 0; k < P; ++k) in[k] = col + k * hop < cols;
+  uint64_t* s_items = reinterpret_cast<uint64_t*>(reinterpret_cast<uint8_t*>(s_raw) + Queue::kSize);
   for (int i = tid; i < (int)blockDim.y * kWindow; i += threads) {
     const int64_t at = ((int64_t)blockIdx.x * blockDim.y + i / kWindow - 1) * kEmbChunk + i % kWindow - 1;
     s_items[i] = at >= 0 && at < a.n ? a.items[at] : ~0ull;
   }
   __syncthreads();
   const int64_t chunk = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-  if (chunk >= a.chunks || col >= a.cols) return;
+  if (chunk >= a.chunks || !in[0]) return;
   const int64_t first = chunk * kEmbChunk;
   const uint64_t* items = s_items + threadIdx.y * kWindow + kEmbChunk + 1;      // of this chunk; a chunk and one token before, two chunks behind
   auto id_at = [&](int i) { return (uint32_t)(items[i] >> 32); };
@@ -421,38 +435,60 @@ __global__ void __launch_bounds__(kEmbThreads, 4) emb_sum_kernel(const __grid_co
   while (begin < end && id_at(end - 1) >= (uint32_t)a.rows) --end;             // tokens that are left out come last
   if (begin >= end) return;
   const T* dout = static_cast<const T*>(a.dout) + col;
-  RowQueue<T, VEC, kEmbAhead> queue{reinterpret_cast<Pack<T, VEC>*>(s_raw) + tid, threads};
+  Queue queue{reinterpret_cast<uint8_t*>(s_raw) + tid * Queue::kCell};
+  auto fetch = [&](int i, int turn) {
+    const uint32_t token = (uint32_t)items[i];
+    const T* row = dout + (int64_t)token * a.ld;
+    const bool edge = token == 0u || token == (uint32_t)(a.n - 1);
+#pragma unroll
+    for (int k = 0; k < P; ++k) if (in[k]) queue.put(turn, k, row + k * hop, edge);
+  };
 #pragma unroll
   for (int i = 0; i < kEmbAhead - 1; ++i) {
-    if (begin + i < end) queue.put(i, dout + (int64_t)(uint32_t)items[begin + i] * a.ld);
+    if (begin + i < end) fetch(begin + i, i);
     queue.close();
   }
-  float acc[VEC];
+  float acc[P][VEC];
+  auto clear = [&] {
 #pragma unroll
-  for (int j = 0; j < VEC; ++j) acc[j] = 0.0f;
+    for (int k = 0; k < P; ++k) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) acc[k][j] = 0.0f;
+    }
+  };
+  clear();
   uint32_t run = id_at(begin);
   bool part = head_part && begin == 0;
   auto flush = [&](int slot) {
-    if (slot >= 0) {
-      float* p = a.parts + (chunk * 2 + slot) * a.ld_part + col;
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) p[j] = acc[j];
-    } else put_row<VEC>(a, a.out + (int64_t)run * a.ld_out + col, acc);
+    for (int k = 0; k < P; ++k) {
+      if (!in[k]) continue;
+      if (slot >= 0) {
+        float* p = a.parts + (chunk * 2 + slot) * a.ld_part + col + k * hop;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) p[j] = acc[k][j];
+      } else put_row<VEC>(a, a.out + (int64_t)run * a.ld_out + col + k * hop, acc[k]);
+    }
   };
+  int turn = 0;
   for (int i = begin; i < end; ++i) {
-    const int ahead = i + kEmbAhead - 1;
-    if (ahead < end) queue.put(ahead - begin, dout + (int64_t)(uint32_t)items[ahead] * a.ld);
+    if (i + kEmbAhead - 1 < end) fetch(i + kEmbAhead - 1, turn == 0 ? kEmbAhead - 1 : turn - 1);
     queue.close();
-    const Pack<T, VEC> x = queue.get(i - begin);
+    queue.wait();
     const uint32_t id = id_at(i);
     if (id != run) {
       flush(part ? 0 : -1);
       run = id; part = false;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) acc[j] = 0.0f;
+      clear();
     }
+    const uint32_t low = (uint32_t)reinterpret_cast<uintptr_t>(dout) + (uint32_t)items[i] * (uint32_t)a.ld * (uint32_t)sizeof(T);      // (of all packs: the hop is a multiple of four bytes)
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) acc[j] += to_float(x.v[j]);
+    for (int k = 0; k < P; ++k) {
+      const Pack<T, VEC> x = queue.get(turn, k, low);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) acc[k][j] += to_float(x.v[j]);
+    }
+    turn = turn + 1 == kEmbAhead ? 0 : turn + 1;
   }
   flush(part ? 0 : tail_part ? 1 : -1);
 }
@@ -722,8 +758,9 @@ struct SortLaunch {
 
 template <typename T, int VEC>
 cudaError_t sum_typed(SumArgs& a, cudaStream_t st) {
-  const EmbShape s = emb_shape(a.cols, VEC);
-  const size_t smem = (size_t)kEmbAhead * s.cx * s.cy * VEC * sizeof(T) + (size_t)s.cy * kWindow * 8;
+  using Queue = RowQueue<T, VEC, kEmbAhead>;
+  const EmbShape s = emb_shape(a.cols, VEC * Queue::kPacks);
+  const size_t smem = Queue::kSize + (size_t)s.cy * kWindow * 8;
   return launch_after(emb_sum_kernel<T, VEC>, dim3((unsigned)((a.chunks + s.cy - 1) / s.cy), s.slabs), dim3(s.cx, s.cy), smem, st, a);
 }
 template <typename T>
