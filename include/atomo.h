@@ -333,7 +333,7 @@ int atomo_embedding_backward(atomo_ctx* ctx, const void* ids /*DEVICE*/, int32_t
  * leading dimensions; weight and bias (either may be NULL: ones, zeros) cols values of weight_type; mean and rstd fp32[rows] are kept for the
  * backward pass, which gives dx (rows x cols of `type`) and, where not NULL, the sums over the rows dweight and dbias (fp32[cols]).
  * y may be x, and dx may be dy or x (same leading dimension).  A row's variance has to lie in the range of fp32.  0 <= rows <= 2^30, 1 <= cols <= 2^22, eps >= 0.
- * workspace: atomo_layer_norm_workspace_bytes (0, and NULL will do, for a few rows; -1 on bad arguments).                           */
+ * workspace: atomo_layer_norm_workspace_bytes (0, and NULL will do, for few rows; -1 on bad arguments).                           */
 int atomo_layer_norm(atomo_ctx* ctx, const void* x /*DEVICE*/, int32_t type, int64_t rows, int64_t cols, int64_t ld, const void* weight /*DEVICE or NULL*/,
                      const void* bias /*DEVICE or NULL*/, int32_t weight_type, double eps, void* y /*DEVICE*/, int64_t ld_y, float* mean /*DEVICE*/,
                      float* rstd /*DEVICE*/, void* stream);

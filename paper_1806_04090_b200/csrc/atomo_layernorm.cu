@@ -5,7 +5,7 @@
 //
 // One pass over memory in either direction: a row stays on chip with one group of threads (a warp, or a CTA), each of which owns the
 // same columns in every row that its group takes, so that the weights are loaded once and the sums of dw and db stay in registers
-// too; the groups' sums are then added by a second kernel, in a fixed order.  The rows to come are copied to shared memory meanwhile, by the threads that
+// too; the groups' sums are then added by a second kernel (of a few rows: inside a cluster), in a fixed order.  The rows to come are copied to shared memory meanwhile, by the threads that
 // will use them, so that copies in flight take no registers and are waited for by their own thread alone; rows that are not aligned are copied in whole 16 bytes
 // all the same and shared by the group.  A thread has up to 16 columns, two at a time in packed
 // fp32: what a row costs every warp (shuffles, the exchange among warps) outweighs the arithmetic where a thread has few, and instruction issue then bounds
@@ -26,6 +26,7 @@ constexpr int kGroupMax = 512;                                   // threads per 
 constexpr int kNormCols = kGroupMax * 16;
 constexpr int kCtaThreads = 256;                                 // of a CTA with several groups side by side
 constexpr int kBackCtas = 148 * 4;                               // partial rows of dw and db, at most
+constexpr int kMates = 8;                                        // CTAs of a cluster that adds them itself, at most
 // By the bytes of a row that a thread has (up to 64): rows per step; steps whose rows are in shared memory or on the way there
 constexpr int kForwardStages = 4, kBackwardStages = 3;
 __host__ __device__ constexpr int rows_per_step(int bytes) { return bytes <= 32 ? 2 : 1; }
@@ -63,6 +64,14 @@ struct Place {
     mate = group * (width >> 5) + at;
   }
 };
+__device__ __forceinline__ void cluster_meet() { asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ float4 remote_values(const float* p, int rank) {
+  uint32_t a = (uint32_t)__cvta_generic_to_shared(p);
+  float4 v;
+  asm("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(a) : "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
+  return v;
+}
 __device__ __forceinline__ float one_over_root(float x) {        // to about one unit in the last place
   const float r = rsqrtf(x);
   return fmaf(r * 0.5f, fmaf(-x * r, r, 1.0f), r);
@@ -307,7 +316,7 @@ __global__ void __launch_bounds__(CTA, 512 / CTA) ln_forward_kernel(int group_wi
 template <typename T, int VEC, int PACKS, int CTA>
 __global__ void __launch_bounds__(CTA, 512 / CTA) ln_backward_kernel(int group_width, const T* dy, int64_t ld_dy, const T* x, int64_t ld_x, int64_t rows, int cols,
                                                                 Weight weight, const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                                T* dx, int64_t ld_dx, float* __restrict__ parts_w, float* __restrict__ parts_b) {
+                                                                T* dx, int64_t ld_dx, float* __restrict__ parts_w, float* __restrict__ parts_b, int mates) {
   constexpr int E = VEC * PACKS, R = rows_per_step(E * sizeof(T)), kStages = kBackwardStages;
   extern __shared__ uint4 s_ring[];                              // afterwards, of several groups: [groups][2][cols] floats
   __shared__ float2 s_sum[2][R][16];
@@ -404,10 +413,11 @@ __global__ void __launch_bounds__(CTA, 512 / CTA) ln_backward_kernel(int group_w
     stage = stage + 1 == kStages ? 0 : stage + 1;
     low_x += (uint32_t)step_x * (uint32_t)sizeof(T); low_dy += (uint32_t)step_dy * (uint32_t)sizeof(T); to += step_dx;
   }
-  // this CTA's rows of partial sums: dw, then db
-  float* part_w = parts_w ? parts_w + (int64_t)blockIdx.x * cols : nullptr;        // (null: a result that is not asked for)
-  float* part_b = parts_b ? parts_b + (int64_t)blockIdx.x * cols : nullptr;
-  if (beside > 1) {
+  // the columns' sums.  Of one CTA, or of a cluster of `mates` that adds them through distributed shared memory: the results; else this CTA's rows of partial sums
+  const int64_t row = mates > 1 ? 0 : (int64_t)blockIdx.x * cols;
+  float* part_w = parts_w ? parts_w + row : nullptr;             // (null: a result that is not asked for)
+  float* part_b = parts_b ? parts_b + row : nullptr;
+  if (beside > 1 || mates > 1) {
     asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();                                             // the ring is no longer read
     float* s_cols = reinterpret_cast<float*>(s_ring);
@@ -415,11 +425,31 @@ __global__ void __launch_bounds__(CTA, 512 / CTA) ln_backward_kernel(int group_w
     put_columns<VEC, PACKS>(mine, width, lane, in, dw);
     put_columns<VEC, PACKS>(mine + cols, width, lane, in, db);
     __syncthreads();
-    for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) {
-      float t = 0.0f;
-      for (int v = 0; v < beside; ++v) t += s_cols[v * 2 * cols + c];
+    auto put = [&](int c, float t) {
       float* part = c < cols ? part_w : part_b;
       if (part) part[c < cols ? c : c - cols] = t;
+    };
+    if (beside > 1) {
+      for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) {
+        float t = 0.0f;
+        for (int v = 0; v < beside; ++v) t += s_cols[v * 2 * cols + c];
+        if (mates > 1) s_cols[c] = t; else put(c, t);
+      }
+    }
+    if (mates > 1) {
+      cluster_meet();
+      for (int c = (blockIdx.x * blockDim.x + threadIdx.x) * 4; c < 2 * cols; c += mates * blockDim.x * 4) {
+        float4 v[kMates];
+#pragma unroll
+        for (int k = 0; k < kMates; ++k) if (k < mates) v[k] = remote_values(s_cols + c, k);          // (all on their way at a time)
+        float4 t = v[0];
+#pragma unroll
+        for (int k = 1; k < kMates; ++k) if (k < mates) { t.x += v[k].x; t.y += v[k].y; t.z += v[k].z; t.w += v[k].w; }
+        const float f[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (c + e < 2 * cols) put(c + e, f[e]);
+      }
+      cluster_meet();                                            // nobody leaves while its shared memory is read
     }
   } else {
     if (part_w) put_columns<VEC, PACKS>(part_w, width, lane, in, dw);
@@ -575,11 +605,19 @@ int resident(const void* kernel, int threads, size_t smem, std::atomic<int> (&kn
   return 148 * std::max(1, std::min(n, (int)(227 * 1024 / (smem + 2048))));
 }
 
-// threads of a group, of a CTA
+// threads of a group (the same whatever the type: 16 columns each, or a warp), of a CTA
 struct Shape { int width, threads; };
-template <int COLUMNS> Shape shape_of(int64_t cols) {
-  const int width = (int)((cols + 32 * COLUMNS - 1) / (32 * COLUMNS)) * 32;
+Shape shape_of(int64_t cols) {
+  const int width = (int)((cols + 511) / 512) * 32;
   return Shape{width, width <= kCtaThreads ? kCtaThreads / width * width : width};
+}
+// A backward pass in one launch, by a cluster whose CTAs add the columns' sums themselves: while each takes about a step (narrow rows: four).  Without the second
+// launch and the workspace a call takes 3.7 us less of the host; kernels, us, one | two launches: 250 x 64 bf16 4.9 | 4.3, 32 x 1023 fp32 8.0 | 7.8, 8 x 4096 fp32 5.9 | 6.4,
+// 8 x 8192 bf16 10 | 21 (there by one CTA, four steps); more rows: 250 x 512 fp32 8.4 | 5.4, 128 x 1023 fp32 16 | 8.
+bool one_launch(int64_t rows, int64_t cols) {
+  if (cols > kNormCols) return false;
+  const Shape s = shape_of(cols);
+  return rows <= (int64_t)kMates * (cols <= 128 ? 4 : 1) * (s.threads / s.width);
 }
 
 template <typename T, int VEC, int PACKS, int CTA>
@@ -595,7 +633,7 @@ cudaError_t forward_cta(const NormForward& a, Shape s, cudaStream_t st) {
 }
 template <typename T, int VEC, int PACKS>
 cudaError_t forward_form(const NormForward& a, cudaStream_t st) {
-  const Shape s = shape_of<VEC * PACKS>(a.cols);
+  const Shape s = shape_of(a.cols);
   if constexpr (VEC * PACKS == 16) { if (s.threads > kCtaThreads) return forward_cta<T, VEC, PACKS, kGroupMax>(a, s, st); }
   return forward_cta<T, VEC, PACKS, kCtaThreads>(a, s, st);
 }
@@ -622,19 +660,29 @@ template <typename T, int VEC, int PACKS, int CTA>
 cudaError_t backward_cta(const NormBackward& a, Shape s, cudaStream_t st) {
   constexpr int R = rows_per_step(VEC * PACKS * (int)sizeof(T));
   const int beside = s.threads / s.width;
-  const size_t smem = std::max<size_t>(Ring<T, VEC, PACKS, 2 * R, kBackwardStages, CTA>::bytes(beside, (int)a.cols), beside > 1 ? (size_t)beside * 2 * a.cols * 4 : 0);
+  const size_t smem = std::max<size_t>(Ring<T, VEC, PACKS, 2 * R, kBackwardStages, CTA>::bytes(beside, (int)a.cols), (size_t)beside * 2 * a.cols * 4 + 16);       // (sums are read four at a time)
   static std::atomic<int> known[17];
-  // a few steps: one CTA, whose sums are the results (the join is a launch, and 3 us)
-  const bool one = a.rows <= 4 * beside * R;
-  const int grid = one ? 1 : std::min(back_ctas(a.rows, (int64_t)beside * R), resident((const void*)ln_backward_kernel<T, VEC, PACKS, CTA>, s.threads, smem, known));
-  ln_backward_kernel<T, VEC, PACKS, CTA><<<grid, s.threads, smem, st>>>(s.width, (const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, a.rows, (int)a.cols, Weight{a.weight, a.weight_type}, a.mean, a.rstd,
-                                                                        (T*)a.dx, a.ld_dx, one ? a.dweight : a.ws, one ? a.dbias : a.ws + (int64_t)grid * a.cols);
-  const cudaError_t e = cudaGetLastError();
-  return e != cudaSuccess || one ? e : backward_join(a, grid, st);
+  auto launch = [&](int grid, int mates, float* w, float* b) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = mates; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(s.threads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.attrs = attr; cfg.numAttrs = mates > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, ln_backward_kernel<T, VEC, PACKS, CTA>, s.width, (const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, a.rows, (int)a.cols,
+                              Weight{a.weight, a.weight_type}, a.mean, a.rstd, (T*)a.dx, a.ld_dx, w, b, mates);
+  };
+  if (one_launch(a.rows, a.cols)) {
+    const int mates = (int)std::min<int64_t>((a.rows + beside * R - 1) / (beside * R), kMates);
+    return launch(mates, mates, a.dweight, a.dbias);
+  }
+  const int grid = std::min(back_ctas(a.rows, (int64_t)beside * R), resident((const void*)ln_backward_kernel<T, VEC, PACKS, CTA>, s.threads, smem, known));
+  const cudaError_t e = launch(grid, 1, a.ws, a.ws + (int64_t)grid * a.cols);
+  return e != cudaSuccess ? e : backward_join(a, grid, st);
 }
 template <typename T, int VEC, int PACKS>
 cudaError_t backward_form(const NormBackward& a, cudaStream_t st) {
-  const Shape s = shape_of<VEC * PACKS>(a.cols);
+  const Shape s = shape_of(a.cols);
   if constexpr (VEC * PACKS == 16) { if (s.threads > kCtaThreads) return backward_cta<T, VEC, PACKS, kGroupMax>(a, s, st); }
   return backward_cta<T, VEC, PACKS, kCtaThreads>(a, s, st);
 }
@@ -684,7 +732,7 @@ int launch_layer_norm(const NormForward& a, cudaStream_t st) {
 }
 
 uint64_t layer_norm_workspace(int64_t rows, int64_t cols) {
-  if (rows <= 4 && cols <= kNormCols) return 0;                  // one CTA, whatever the type
+  if (one_launch(rows, cols)) return 0;
   return (uint64_t)std::min<int64_t>(rows, kBackCtas) * 2 * cols * 4;
 }
 

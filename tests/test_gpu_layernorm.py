@@ -82,6 +82,29 @@ def test_heights(atomo, rows, cols, dtype):
     _check(atomo, x, dy, torch.randn(cols, generator=gen, device="cuda"), torch.randn(cols, generator=gen, device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("cols,limit", [(3, 256), (128, 256), (129, 64), (512, 64), (513, 32), (1023, 32), (1536, 16), (2048, 16), (4095, 8), (8192, 8)])
+def test_rows_that_one_launch_takes(atomo, cols, limit, dtype):
+    """Up to `limit` rows the weight's gradient is added inside one launch, without a workspace; a result that is not asked for is left out."""
+    size = atomo.lib.atomo_layer_norm_workspace_bytes
+    assert size(limit, cols) == 0 and size(limit + 1, cols) > 0
+    gen = _gen(6)
+    w = torch.randn(cols, generator=gen, device="cuda")
+    for rows in (limit // 8, limit // 2 + 1, limit, limit + 1):
+        x, dy = _input(rows, cols, dtype, gen), torch.randn(rows, cols, generator=gen, device="cuda").to(dtype)
+        _check(atomo, x, dy, w, w)
+    x, dy = x[:limit], dy[:limit]
+    _, mean, rstd = atomo.atomo_layer_norm(x, w, w)
+    dx, dw, db = atomo.atomo_layer_norm_backward(dy, x, w, mean, rstd)
+    kind = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}[dtype]
+    for want_w in (True, False):
+        got, room = torch.empty_like(dx), torch.full((2, cols), 7.0, device="cuda")
+        args = (dy.data_ptr(), cols, x.data_ptr(), cols, kind, limit, cols, w.data_ptr(), 0, mean.data_ptr(), rstd.data_ptr(), got.data_ptr(), cols)
+        assert atomo.lib.atomo_layer_norm_backward(atomo._h, *args, room[0].data_ptr() if want_w else None, None if want_w else room[1].data_ptr(), None, 0, None) == 0
+        torch.cuda.synchronize()
+        assert torch.equal(got, dx) and torch.equal(room[0], dw if want_w else torch.full_like(dw, 7.0)) and torch.equal(room[1], torch.full_like(db, 7.0) if want_w else db)
+
+
 def test_without_weight_or_bias(atomo):
     gen = _gen(3)
     for cols in (40, 3000, 9000):

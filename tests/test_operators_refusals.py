@@ -93,15 +93,15 @@ def test_layer_norm(ctx):
         assert forward(**bad) == INVALID, bad
 
     size = lib.atomo_layer_norm_workspace_bytes
-    assert size(3, 4) == 0 and size(100, 4) > 0 and size(3, 100000) > 0 and size(-1, 4) == size(3, 0) == size((1 << 30) + 1, 4) == -1
+    assert size(3, 4) == size(256, 4) == 0 and size(257, 4) > 0 and size(1000, 4) > 0 and size(3, 100000) > 0 and size(-1, 4) == size(3, 0) == size((1 << 30) + 1, 4) == -1
 
     def backward(dy=GOOD, ld_dy=4, x=GOOD, ld_x=4, kind=0, rows=3, cols=4, w=GOOD, wkind=0, mean=GOOD, rstd=GOOD, dx=GOOD, ld_dx=4, dw=GOOD, db=GOOD, ws=GOOD, nbytes=1 << 30):
         return lib.atomo_layer_norm_backward(h, dy, ld_dy, x, ld_x, kind, rows, cols, w, wkind, mean, rstd, dx, ld_dx, dw, db, ws, nbytes, None)
 
     for bad in (dict(dy=None), dict(ld_dy=3), dict(x=None), dict(x=GOOD + 2), dict(ld_x=3), dict(kind=4), dict(rows=-1), dict(cols=0), dict(w=GOOD + 2), dict(wkind=-1), dict(mean=None),
-                dict(rstd=GOOD + 2), dict(dx=None), dict(ld_dx=2), dict(dw=GOOD + 2), dict(db=GOOD + 1), dict(rows=100, ws=None), dict(rows=100, ws=GOOD + 4)):
+                dict(rstd=GOOD + 2), dict(dx=None), dict(ld_dx=2), dict(dw=GOOD + 2), dict(db=GOOD + 1), dict(rows=1000, ws=None), dict(rows=1000, ws=GOOD + 4)):
         assert backward(**bad) == INVALID, bad
-    assert backward(rows=100, nbytes=size(100, 4) - 1) == CAPACITY
+    assert backward(rows=1000, nbytes=size(1000, 4) - 1) == CAPACITY
 
 
 def test_adamw_state_checks_its_tensors():
