@@ -40,7 +40,7 @@ EmbShape emb_shape(int64_t cols, int vec) {
   EmbShape s;
   if (packs <= kEmbThreads / 2) {
     s.cx = 8;                                                    // at most 32 rows, whose chunks' items take 25 KB of shared memory
-    while (s.cx < packs) s.cx <<= 1;
+    while (s.cx < packs) s.cx += s.cx < 32 ? s.cx : 32;           // (warps that are full as far as can be)
     s.cy = kEmbThreads / s.cx; s.slabs = 1;
   } else {
     s.slabs = (int)((packs + kEmbThreads - 1) / kEmbThreads);
