@@ -282,7 +282,8 @@ int atomo_grad_norm(atomo_ctx* ctx, const atomo_tensor* grads /*HOST array*/, in
  *   m = beta1 m + (1 - beta1) c g,  v = beta2 v + (1 - beta2) (c g)^2,
  *   p = p - lr weight_decay p - lr / (1 - beta1^step) m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
  * with c = scale[1] (DEVICE, as atomo_grad_norm leaves it; NULL: c = 1).  A c that is not finite leaves every parameter and state as
- * it is.  grads[i] belongs to tensors[i] and has n elements of grad_type.  With `master` the fp32 copy is what is
+ * it is.  Both moments are fp32 operations, each rounded once: (beta1 m) + ((1 - beta1) (c g)), (beta2 v) + (((1 - beta2) (c g)) (c g)), the constants rounded to fp32.
+ * grads[i] belongs to tensors[i] and has n elements of grad_type.  With `master` the fp32 copy is what is
  * updated, and param receives it rounded; without it param is read and written in its own type.
  *   State in 32 bits: exp_avg and exp_avg_sq are fp32[n], the scales NULL.
  *   State in 8 bits: exp_avg and exp_avg_sq are OCP e4m3 numbers, one byte each; exp_avg_scale and exp_avg_sq_scale hold one byte

@@ -76,6 +76,7 @@ int launch_grad_norm(const atomo_tensor* grads, int n, double max_norm, float* o
 // ---- AdamW (atomo_step.cu) ------------------------------------------------------------------------
 struct AdamHyper {
   float beta1, one_minus_beta1, beta2, one_minus_beta2;
+  float one = 1.0f;                           // a one that the kernels' compiler does not know
   float lr, step_size, inv_root_bias2, eps;   // step_size = lr / (1 - beta1^t), inv_root_bias2 = 1 / sqrt(1 - beta2^t)
   const float* scale;                         // DEVICE: {norm, factor of the gradient}, or null
   uint32_t step; int32_t grad_type;

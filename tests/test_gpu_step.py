@@ -303,6 +303,44 @@ def test_8_bit_states_follow_a_decaying_average(atomo):
     assert abs(v.mean() / want - 1) < 5 * math.sqrt(300 * 0.005 / 8 / n) * 2
 
 
+def _moments_in_fp32(m, v, g, c, beta1, beta2):
+    """The moments of a step, each operation rounded once."""
+    b1, r1, b2, r2 = (np.float32(x) for x in (beta1, 1.0 - beta1, beta2, 1.0 - beta2))
+    g = g.astype(np.float32) * np.float32(c)
+    return b1 * m.astype(np.float32) + r1 * g, b2 * v.astype(np.float32) + r2 * g * g
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("shift", [0, 3])
+@pytest.mark.parametrize("c", [1.0, 0.3])
+def test_moments_are_rounded_operation_by_operation(atomo, bits, shift, c):
+    """Bit for bit what the same fp32 operations give, whatever form an element goes through: whole chunks, tails, unaligned tensors."""
+    lengths, seed, step = [60000, 4097, 33], 77, 6
+    state, grads, flats = _case(lengths, torch.float32, torch.float32, bits, False, 23, shift)
+    before = _snapshot(flats)
+    scale = torch.tensor([5.0, c], device="cuda")
+    atomo.atomo_adamw(state, grads, step=step, seed=seed, scale=scale, **HYPER)
+    for i, n in enumerate(lengths):
+        at, ab = slice(shift, shift + n), slice(shift, shift + -(-n // 32))
+        if bits == 32:
+            m, v = (before[k][i][at].cpu().numpy() for k in ("m", "v"))
+        else:
+            m, v = (ref.decode_state(before[k][i][at], before[k + "s"][i][ab]) for k in ("m", "v"))
+        m, v = _moments_in_fp32(m, v, grads[i].cpu().numpy(), float(scale[1]), HYPER["beta1"], HYPER["beta2"])
+        if bits == 32:
+            assert np.array_equal(state.exp_avg[i].cpu().numpy(), m) and np.array_equal(state.exp_avg_sq[i].cpu().numpy(), v)
+        else:
+            words = ref.philox_words(n, i, step, seed)
+            for x, codes, scales, random, keep in ((m, state.exp_avg[i], state.exp_avg_scale[i], words & 0xFFFF, False), (v, state.exp_avg_sq[i], state.exp_avg_sq_scale[i], words >> 16, True)):
+                # x / quantum has 24 bits and the random number 16 behind the point: their sum and its floor are exact in 64 bits.  (A value far below its
+                # block's largest is first cut to 2^-20 of a quantum, to the nearest.)
+                want, quantum, _ = ref.encode_state(x.astype(np.float64), random.astype(np.float64), keep)
+                cut = np.round(x.astype(np.float64) / quantum * 2.0 ** 20) / 2.0 ** 20 * quantum
+                fine = cut == x
+                got = ref.decode_state(codes, scales)
+                assert np.array_equal(got[fine], want[fine]) and fine.mean() > 0.9
+
+
 def test_step_repeats_bit_for_bit_and_follows_its_seed(atomo):
     results = []
     for seed in (7, 7, 8):
