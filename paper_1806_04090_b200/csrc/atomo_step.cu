@@ -329,9 +329,10 @@ __device__ __forceinline__ void state_encode(const float (&x)[PER], const uint32
     byte = (uint32_t)max((int)((top + 0x200000u) >> 23) - 8, 0);
     factor = __uint_as_float(7u << 23);                          // 2^-120
 #pragma unroll
-    for (int j = 0; j < PER; ++j) y[j] *= __uint_as_float((254u - byte) << 23);
+    for (int j = 0; j < PER; ++j) y[j] = __fmul_rn(y[j], __uint_as_float((254u - byte) << 23));
   }
-  // (The product is written as a packed one: with a scalar one the compiler's results were zero here, as tests/test_gpu_step.py shows.)
+  // (No product by `*` here: nvcc 12.9.86 takes the bits of one for zero where they are shifted and added as below, which a kernel of these lines alone
+  // shows; of a packed product, of __fmul_rn and of mul.rn.f32 they are right.  The packed one takes half the instructions.)
   uint32_t t[PER], least = 0xffffffffu;
   const uint64_t factors = pack2(factor, factor);
 #pragma unroll

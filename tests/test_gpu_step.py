@@ -266,6 +266,40 @@ def test_state_in_8_bits_of_values_that_are_not_finite(atomo):
     assert np.all(np.abs(m - want)[fine] <= 2.0 ** -3 * np.abs(want)[fine] * (1 + 1e-5) + np.abs(want[fine]).max() * 2.0 ** -16)
 
 
+@pytest.mark.parametrize("shift", [0, 3])
+def test_state_in_8_bits_of_large_values(atomo, shift):
+    """Blocks with finite moments of 2^13 to 2^15, 1e10 and beyond, of one size or beside small ones, from states with exponent bytes up to 220."""
+    from paper_1806_04090_b200 import api
+    n, step, seed = 8192 + 40, 9, 1234567
+    blocks = -(-n // 32)
+    gen = _gen(24)
+    rand = lambda k: torch.randn(k + 40, generator=gen, device="cuda")  # noqa: E731
+    size = torch.tensor([1e-3, 1.0, 2.0 ** 14, 3e5, 1e7, 1e10, 1e15], device="cuda")[torch.arange(n + 40, device="cuda") // 32 % 7]
+    g = rand(n) * size
+    g[::64 * 3] = 1e15                                    # one large value in a block of another size
+    codes, scales = [], []
+    for top in (220, 190):                                # the second moment's next value stays finite: 448 * 2^63, and 1e30 / 200
+        codes.append((rand(n) * 60).clamp(-448, 448).abs().to(torch.float8_e4m3fn))
+        scales.append(torch.randint(90, top + 1, (blocks + 40,), generator=gen, device="cuda", dtype=torch.int32).to(torch.uint8))
+        scales[-1][::3] = torch.randint(134, 146, (scales[-1][::3].numel(),), generator=gen, device="cuda", dtype=torch.int32).to(torch.uint8)
+        scales[-1][::7] = 0
+    codes[0] = (codes[0].float() * torch.sign(rand(n))).to(torch.float8_e4m3fn)
+    codes, scales = [_odd(c, n, shift) for c in codes], [_odd(c.view(torch.float8_e8m0fnu), blocks, shift) for c in scales]
+    m, v = (ref.decode_state(c, e) for c, e in zip(codes, scales))
+    grads = [_odd(g, n, shift)]
+    state = api.AdamWState([torch.zeros(n, device="cuda")], [codes[0]], [codes[1]], [scales[0]], [scales[1]])
+    atomo.atomo_adamw(state, grads, step=step, seed=seed, **HYPER)
+    m, v = _moments_in_fp32(m, v, grads[0].cpu().numpy(), 1.0, HYPER["beta1"], HYPER["beta2"])
+    assert np.isfinite(m).all() and np.isfinite(v).all() and np.abs(m).max() > 1e29 and (np.abs(m) < 1e-3).any()
+    words = ref.philox_words(n, 0, step, seed)
+    for x, got, random, keep in ((m, ref.decode_state(codes[0], scales[0]), words & 0xFFFF, False), (v, ref.decode_state(codes[1], scales[1]), words >> 16, True)):
+        x, random = x.astype(np.float64), random.astype(np.float64)
+        _, quantum, _ = ref.encode_state(x, random, keep)
+        cut = np.round(x / quantum * 2.0 ** 20) / 2.0 ** 20 * quantum           # what of a value far below its block's largest is looked at
+        want, _, _ = ref.encode_state(np.where(cut == 0, x, cut), random, keep)
+        assert np.array_equal(got, want)
+
+
 def test_8_bit_states_are_unbiased(atomo):
     """The mean over many seeds of a rounded state is the state: within five standard deviations of the mean of so many roundings of one quantum."""
     from paper_1806_04090_b200 import api
