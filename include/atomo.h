@@ -292,6 +292,8 @@ int atomo_grad_norm(atomo_ctx* ctx, const atomo_tensor* grads /*HOST array*/, in
  * average would stand still where a step changes it by less than half a unit), by the Philox words of the conventions
  * above with key = seed and counter = (i>>2 low, 2^31 | i>>2 high, tensor, step & 0x7fffffff), which no encode uses: element i takes the low 16 bits of
  * word i&3 for the first moment, the high ones for the second.  A second moment above zero is not rounded to zero.  A state that is not finite becomes NaN.
+ * An eps below 2^-38 / sqrt(1 - beta2^step) (1.2e-10 in the first step with beta2 = 0.999, later 3.6e-12) takes a form with more care for subnormal numbers, with
+ * 8-bit states half as fast; eps = 0 is such a one.
  * Parameters, states and gradients do not overlap; a parameter may be empty.  Every n < 2^34 with 8-bit states.      */
 enum { ATOMO_STATE_BLOCK = 32 };
 typedef struct {

@@ -708,7 +708,8 @@ class Atomo:
                     eps: float = 1e-8, seed: int = 0, scale: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
         """One AdamW step (decoupled weight decay) over all parameters of `state`, in place.  grads: one contiguous tensor per parameter, all of
         one type.  step counts from 1.  scale: what atomo_grad_norm returned; its second number multiplies the gradients, and where it
-        is not finite nothing is updated.  seed: of the stochastic rounding of 8-bit states."""
+        is not finite nothing is updated.  seed: of the stochastic rounding of 8-bit states.  (An eps below 3.6e-12 / sqrt(1 - beta2^step), zero among them, is served
+        exactly too, with 8-bit states at half the speed.)"""
         if stream is not None:
             return self._on(stream, self.atomo_adamw, state, grads, lr, step, beta1, beta2, eps, seed, scale)
         n, device = len(state.lengths), self.device

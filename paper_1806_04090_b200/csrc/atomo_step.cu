@@ -237,7 +237,8 @@ namespace {
 // all in fp32, the moments' products and sums each rounded once, in the order written here with (1 - b2) (c g) first: a state in 8 bits is what such a
 // moment rounds to, so that an element's codes do not depend on its address, and any other program gets them from the same formula.  c is read from device memory.  A CTA takes kAdamChunk neighbouring elements of a tensor, a thread several groups of
 // neighbouring ones, all loads first.  Chunks that lie inside an aligned tensor go through adam_inside, compiled for the types (with 8-bit states
-// instruction issue bounds the kernel as much as memory does); a tensor's last chunk, and tensors of other alignment, through adam_any.
+// instruction issue bounds the kernel as much as memory does); a tensor's last chunk, tensors of other alignment, other pairs of types and a very small eps through
+// adam_any (25.6M fp32 elements, back to back, us, inside | any: fp32 states 109 | 110, 8-bit states 68 | 129).
 constexpr int kAdamThreads = 256, kAdamChunk = 2048;
 constexpr int kStateBlock = ATOMO_STATE_BLOCK;
 
@@ -267,8 +268,9 @@ __device__ __forceinline__ void adam_element(const AdamHyper& h, float c, float 
 }
 
 // The same for pairs of elements, on packed fp32, without the care for subnormal numbers that root and quotient take: a second moment below 2^-126
-// counts as zero, which is nothing beside an eps of kEpsPairs (1e-19 in 1e-12); smaller ones go through adam_element.
-constexpr float kEpsPairs = 1.0e-12f;
+// counts as zero.  Its root, below 2^-63, is multiplied by inv_root_bias2 before eps is added: beside an eps of kEpsPairs inv_root_bias2 or more that is less
+// than 2^-25 of the sum, half of half a unit.  Calls with a smaller eps go through adam_element.
+constexpr float kEpsPairs = 1.0f / (1ull << 38);                 // 3.6e-12
 struct AdamPairs { uint64_t c, one, b1, r1, b2, r2, inv, eps, decay, step; };
 __device__ __forceinline__ AdamPairs adam_pairs(const AdamHyper& h, float c, float decay) {
   auto both = [](float x) { return pack2(x, x); };
@@ -594,7 +596,7 @@ __global__ void __launch_bounds__(kAdamThreads, 5) adamw_kernel(const __grid_con
   const AdamTensor& t = B.t[lo];
   const AdamHyper& h = B.h;
   const int64_t first = (int64_t)(blockIdx.x - B.chunk0[lo]) * kAdamChunk;
-  if (t.vec && first + kAdamChunk <= t.n && h.eps >= kEpsPairs) {
+  if (t.vec && first + kAdamChunk <= t.n && h.eps >= kEpsPairs * h.inv_root_bias2) {
     const bool same = h.grad_type == t.type, wide = h.grad_type == ATOMO_TYPE_F32, master = t.master != nullptr;
     if (t.type == ATOMO_TYPE_F32) {
       if (!master && wide) return adam_inside<BITS, float, float, false>(t, h, first);

@@ -219,6 +219,25 @@ def test_first_step_from_zero(atomo, bits):
     ref.near(p, -0.1 * np.sign(_np(g)), np.full(5000, 0.1 * 32 * ref.U32))
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("beta2,step", [(0.999, 1), (0.999999, 1), (0.999, 5000)])
+@pytest.mark.parametrize("eps", [1e-13, 1e-12, 4e-12, 1.2e-10, 4e-9])
+def test_small_eps_beside_smaller_moments(atomo, eps, beta2, step, bits):
+    """Second moments on both sides of the smallest normal number, whose roots count beside an eps of this size where the bias is corrected for by a large factor."""
+    from paper_1806_04090_b200 import api
+    n = 6000
+    gen = _gen(25)
+    g = torch.randn(n, generator=gen, device="cuda") * 10.0 ** torch.linspace(-18.0, -14.0, n, device="cuda")
+    if beta2 == 0.999999:
+        g *= 30.0
+    p = torch.zeros(n, device="cuda")
+    state = api.AdamWState.zeros([p], bits=bits, weight_decay=0.0)
+    atomo.atomo_adamw(state, [g], lr=0.1, step=step, beta1=0.9, beta2=beta2, eps=eps, seed=1)
+    (want, _, v), (off, _, _) = ref.adamw(np.zeros(n), _np(g), np.zeros(n), np.zeros(n), 0.1, step, 0.9, beta2, eps, 0.0, 1.0)
+    assert (v < 2.0 ** -126).any() and (v > 2.0 ** -126).any()
+    ref.near(p, want, off)
+
+
 def test_mixed_types_in_one_call(atomo):
     from paper_1806_04090_b200 import api
     gen = _gen(17)
