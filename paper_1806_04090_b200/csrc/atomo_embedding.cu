@@ -198,7 +198,7 @@ template <bool ONE>
 __global__ void __launch_bounds__(kSortThreads, 1) emb_sort_kernel(const __grid_constant__ SortArgs a) {
   extern __shared__ uint64_t s_items[];                          // [kSortTile] the tile in order; ONE: [kSortTile] what the next pass ranks
   uint64_t* s_next = s_items + kSortTile;
-  __shared__ uint16_t s_warp[kSortWarps][256];                   // a digit's items per warp, then before the warp
+  __shared__ __align__(16) uint16_t s_warp[kSortWarps][256];     // a digit's items per warp, then before the warp
   __shared__ uint32_t s_hist[256], s_base[256], s_tile[256], s_first[256], s_scan[2][8];   // s_first: of a digit in the ordered tile
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int64_t begin = min((int64_t)blockIdx.x * a.segment, a.n), end = min(begin + a.segment, a.n);
@@ -556,7 +556,7 @@ template <typename T, int VEC> struct DirectShape {              // columns of a
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kDirectThreads, 2) emb_direct_kernel(const __grid_constant__ DirectArgs a) {
   constexpr int PACKS = DirectShape<T, VEC>::kPacks, COLS = DirectShape<T, VEC>::kCols, kAhead = VEC * sizeof(T) == 16 && sizeof(T) == 2 ? 4 : 8;
-  extern __shared__ uint32_t s_keys[];                           // [padded] row << kDirectBits | token; then [2][warps][COLS] parts of runs, a flag per row
+  extern __shared__ __align__(16) uint32_t s_keys[];             // [padded] row << kDirectBits | token; then [2][warps][COLS] parts of runs, a flag per row
   float* s_part = reinterpret_cast<float*>(s_keys + a.padded);
   uint8_t* s_seen = reinterpret_cast<uint8_t*>(s_part + 2 * kDirectWarps * COLS);
   __shared__ int s_count, s_row[2][kDirectWarps + 1];            // rows of the parts, -1: none
