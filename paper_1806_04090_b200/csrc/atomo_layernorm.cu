@@ -72,9 +72,9 @@ __device__ __forceinline__ float4 remote_values(const float* p, int rank) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
   return v;
 }
-__device__ __forceinline__ float one_over_root(float x) {        // to about one unit in the last place
-  const float r = rsqrtf(x);
-  return fmaf(r * 0.5f, fmaf(-x * r, r, 1.0f), r);
+__device__ __forceinline__ float one_over_root(float x) {        // to about one unit in the last place; of zero Inf, of Inf zero
+  const float r = rsqrtf(x), e = fmaf(-x * r, r, 1.0f);
+  return e == e ? fmaf(r * 0.5f, e, r) : r;
 }
 
 // The rows that come next: STAGES steps of ROWS rows (x, or x and dy by turns) in shared memory, for a group of `width` threads of which this is `lane`.

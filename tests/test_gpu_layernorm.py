@@ -256,3 +256,19 @@ def test_refused_tensors(atomo):
     for bad in (dict(dy=x[:5]), dict(dy=x.half()), dict(mean=s[:5]), dict(rstd=s.half()), dict(rstd=torch.zeros(12, device="cuda")[::2]), dict(weight=torch.ones(9, device="cuda"))):
         with pytest.raises(ValueError):
             atomo.atomo_layer_norm_backward(**{"dy": x, "x": x, "weight": w, "mean": s, "rstd": s, **bad})
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 1), (5, 64), (9, 1023), (40, 2048), (3, 8192), (2, 8200), (4, 16384)])
+def test_rows_without_variance_and_no_eps(atomo, rows, cols, dtype):
+    """rstd is 1 / sqrt(0), and y a zero times that; the rows beside are as they are alone."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(41)
+    x = torch.randn(rows, cols, generator=gen, device="cuda").to(dtype) if cols > 1 else torch.zeros(rows, cols, device="cuda", dtype=dtype)
+    want = atomo.atomo_layer_norm(x, eps=0.0)
+    x[rows // 2] = 3.0 if cols & (cols - 1) == 0 else 0.0          # (sums of which the mean is exact)
+    y, mean, rstd = atomo.atomo_layer_norm(x, eps=0.0)
+    assert float(rstd[rows // 2]) == float("inf") and float(mean[rows // 2]) == float(x[rows // 2, 0]) and bool(y[rows // 2].isnan().all())
+    others = torch.arange(rows, device="cuda") != rows // 2
+    for a, b in zip((y, mean, rstd), want):
+        assert torch.equal(a[others], b[others])
