@@ -219,6 +219,15 @@ _ADAMW_ARGS = struct.Struct("=ddddqQQii").pack          # _AdamWArgs
 _T, _dtype_of = torch.Tensor, operator.attrgetter("dtype")
 
 
+def _no_graph(*tensors) -> None:
+    """Refuses tensors that autograd would follow through a call: the operators record no graph, and a gradient would end there without a word."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise RuntimeError("the operators record no autograd graph, but one of the tensors requires a gradient: detach it, or make the call under "
+                                   "torch.no_grad() or in the methods of a torch.autograd.Function")
+
+
 def default_k_cap(s: float, n_atoms: int) -> int:
     """k is a sum of independent Bernoulli draws with mean <= s: s + 8 sqrt(s) + 8 is never reached."""
     return int(min(n_atoms, np.ceil(s + 8.0 * np.sqrt(max(float(s), 0.0)) + 8.0)))
@@ -648,6 +657,7 @@ class Atomo:
         return [float(x) for x in out]
 
     # ---- operators on either side of the exchange ---------------------------------------------
+    # They record no autograd graph: the embedding, the layer norm and their gradients refuse tensors that require a gradient where one would be recorded.
     # (Small calls take as long as their host side: what is a C call on a tensor, an allocation or a ctypes object is counted here.)
     def _on(self, stream: torch.cuda.Stream, call, *args):
         """A call with `stream` current, so that what it allocates belongs to that stream too."""
@@ -746,6 +756,7 @@ class Atomo:
         if stream is not None:
             return self._on(stream, self.atomo_embedding, table, ids, scale, out, status)
         kind = self._operand(table, "table").dtype
+        _no_graph(table, out)
         if table.dim() != 2:
             raise ValueError("table: a matrix is required")
         rows, cols = table.shape
@@ -772,6 +783,7 @@ class Atomo:
         if stream is not None:
             return self._on(stream, self.atomo_embedding_backward, ids, grad, rows, scale, padding_idx, out, accumulate, status)
         code = TYPE_CODES[self._operand(grad, "grad").dtype]
+        _no_graph(grad, out)
         width = self._ids(ids)
         if grad.dim() < 1 or grad.shape[:-1] != ids.shape:
             raise ValueError("grad: the shape of ids with one more dimension is required")
@@ -812,6 +824,7 @@ class Atomo:
         if stream is not None:
             return self._on(stream, self.atomo_layer_norm, x, weight, bias, eps, out)
         kind = self._operand(x, "x").dtype
+        _no_graph(x, weight, bias, out)
         shape = x.shape
         cols = shape[-1] if shape else 0
         w, wkind = self._weight(weight, cols, "weight")
@@ -840,6 +853,7 @@ class Atomo:
             return self._on(stream, self.atomo_layer_norm_backward, dy, x, weight, mean, rstd, out)
         kind = self._operand(x, "x").dtype
         self._operand(dy, "dy", (kind,))
+        _no_graph(dy, x, weight, out)
         shape = x.shape
         cols = shape[-1] if shape else 0
         if dy.shape != shape:
