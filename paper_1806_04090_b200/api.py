@@ -219,6 +219,10 @@ _ADAMW_ARGS = struct.Struct("=ddddqQQii").pack          # _AdamWArgs
 _T, _dtype_of = torch.Tensor, operator.attrgetter("dtype")
 
 
+# autograd's check of saved tensors sees what a call writes through a raw pointer only when told (takes tensors; those of inference mode are left out)
+_written = torch._C._increment_version
+
+
 def _no_graph(*tensors) -> None:
     """Refuses tensors that autograd would follow through a call: the operators record no graph, and a gradient would end there without a word."""
     if torch.is_grad_enabled():
@@ -705,6 +709,8 @@ class Atomo:
             out = self._floats.new_empty(2)
         elif not (out.get_device() == device and out.dtype == torch.float32 and out.numel() == 2 and out.is_contiguous()):
             raise ValueError(f"out: two fp32 numbers on CUDA device {device} are required")
+        else:
+            _written((out,))
         s = self._own_stream()
         packed = struct.pack("=%dq" % (3 * n), *desc)
         nbytes = self.lib.atomo_grad_norm_workspace_bytes(packed, n)
@@ -735,6 +741,7 @@ class Atomo:
             raise ValueError(f"scale: two fp32 numbers on CUDA device {device} are required")
         args = _ADAMW_ARGS(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, 0 if scale is None else scale.data_ptr(), state.bits, TYPE_CODES[kind])
         rc = self.lib.atomo_adamw(self._h, state._desc, struct.pack("=%dQ" % n, *map(_T.data_ptr, grads)), n, args, self._own_stream())
+        _written(state.params)
         self._check(rc, "atomo_adamw")
 
     def _status(self, status: Optional[torch.Tensor]):
@@ -770,6 +777,7 @@ class Atomo:
             n_out, ld_out = _rows(self._operand(out, "out", (kind,)), cols, "out")
             if n_out != n:
                 raise ValueError(f"out: {n} rows are required")
+            _written((out,))
         rc = self.lib.atomo_embedding(self._h, table.data_ptr(), TYPE_CODES[kind], rows, cols, ld, ids.data_ptr(), width, n, scale, out.data_ptr(), ld_out,
                                       self._status(status) if status is not None else None, self._own_stream())
         self._check(rc, "atomo_embedding")
@@ -798,6 +806,7 @@ class Atomo:
             n_out, ld_out = _rows(self._operand(out, "out", (torch.float32,)), cols, "out")
             if n_out != rows:
                 raise ValueError(f"out: {rows} rows are required")
+            _written((out,))
         s = self._own_stream()
         nbytes = self.lib.atomo_embedding_workspace_bytes(n, rows, cols)
         if nbytes < 0:
@@ -838,6 +847,7 @@ class Atomo:
             if self._operand(out, "out", (kind,)).shape != shape:
                 raise ValueError("out: the shape of x is required")
             ld_out = cols if out.is_contiguous() else _rows(out, cols, "out")[1]
+            _written((out,))
         lines = rows if len(shape) == 2 else shape[:-1]
         mean, rstd = self._floats.new_empty(lines), self._floats.new_empty(lines)
         rc = self.lib.atomo_layer_norm(self._h, x.data_ptr(), TYPE_CODES[kind], rows, cols, ld, w, b, TYPE_CODES[wkind or bkind or kind], eps, out.data_ptr(), ld_out,
@@ -870,6 +880,7 @@ class Atomo:
             if self._operand(out, "out", (kind,)).shape != shape:
                 raise ValueError("out: the shape of x is required")
             ld_dx = cols if out.is_contiguous() else _rows(out, cols, "out")[1]
+            _written((out,))
         dweight, dbias = self._floats.new_empty(cols), self._floats.new_empty(cols)
         s = self._own_stream()
         nbytes = self.lib.atomo_layer_norm_workspace_bytes(rows, cols)

@@ -93,3 +93,31 @@ def test_inside_an_autograd_function(atomo, data):
         sizes = [torch.zeros_like(t).index_add_(0, data["ids"], dx * 0.5), (dy * hat).sum(0), dy.sum(0)]
     for g, e, size in zip(got, exact, sizes):
         assert bool(((g.double() - e).abs() <= 320 * 2.0 ** -24 * size).all())
+
+
+def test_what_a_call_writes_counts_as_changed(atomo, data):
+    """A tensor that autograd has saved and a call has written over is found out by the backward pass."""
+    from paper_1806_04090_b200 import api
+    p = data["table"].clone().requires_grad_(True)
+    state = api.AdamWState.zeros([p], bits=8)
+    loss = (p * p).sum()
+    atomo.atomo_adamw(state, [torch.ones_like(p)], lr=0.1, step=1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    for call, tensors in _calls(atomo, data):
+        out = tensors[-1]
+        w = torch.ones_like(out).requires_grad_(True)
+        loss = (w * out).sum()
+        call(*tensors)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    out = torch.zeros(2, device="cuda")
+    w = torch.ones(2, device="cuda", requires_grad=True)
+    loss = (w * out).sum()
+    atomo.atomo_grad_norm([data["dy"]], out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():                         # tensors without a version
+        q = torch.zeros(64, device="cuda")
+        atomo.atomo_adamw(api.AdamWState.zeros([q]), [torch.ones(64, device="cuda")], lr=0.1, step=1)
+        assert float(q.max()) < 0.0
