@@ -386,8 +386,8 @@ class AdamWState:
     elements.  State in 8 bits: float8_e4m3fn tensors of as many elements, with exp_avg_scale and exp_avg_sq_scale of one
     float8_e8m0fnu number for each 32 elements.  master: fp32 copies that are updated instead of the parameters, which then receive them
     rounded (None, or a list in which single entries may be None).  weight_decay: one number, or one per parameter.
-    The object keeps the tensors and describes their memory once: they are updated in place and must not be given
-    other memory.  `AdamWState.zeros(params, bits=...)` makes the states of a new run."""
+    The object keeps the tensors and their memory and describes it once: they are updated in place.  A parameter that was given other memory since
+    (p.data = ..., a module moved or cast) is refused by the call; states must not be given other memory.  `AdamWState.zeros(params, bits=...)` makes the states of a new run."""
 
     def __init__(self, params: Sequence[torch.Tensor], exp_avg: Sequence[torch.Tensor], exp_avg_sq: Sequence[torch.Tensor],
                  exp_avg_scale: Optional[Sequence[torch.Tensor]] = None, exp_avg_sq_scale: Optional[Sequence[torch.Tensor]] = None,
@@ -434,6 +434,10 @@ class AdamWState:
             raise ValueError("parameters and states must not overlap")
         self.device = dev
         self._desc = (_AdamWTensor * n)(*desc)
+        # what the description names stays allocated, also where one of the tensors is given other memory
+        self._memory = [t.detach() for part in lists[:5] + (self.params,) for t in part if t is not None]
+        self._addresses = [d[0] for d in desc]
+        self._pack = struct.Struct("=%dQ" % n).pack
 
     @classmethod
     def zeros(cls, params: Sequence[torch.Tensor], bits: int = 32, master: bool = False, weight_decay=0.01) -> "AdamWState":
@@ -733,6 +737,8 @@ class Atomo:
             raise ValueError(f"{n} gradients are required")
         if state.device.index != device:
             raise ValueError(f"the parameters are on {state.device}, the context on device {device}")
+        if list(map(_T.data_ptr, state.params)) != state._addresses:
+            raise ValueError("a parameter was given other memory since its AdamWState was made: make one of the parameters as they are, with the same states")
         kind = grads[0].dtype
         if not (kind in TYPE_CODES and set(map(_dtype_of, grads)) == {kind} and set(map(_T.get_device, grads)) == {device} and list(map(_T.numel, grads)) == state.lengths
                 and all(map(_T.is_contiguous, grads))):
@@ -740,7 +746,7 @@ class Atomo:
         if scale is not None and not (scale.get_device() == device and scale.dtype == torch.float32 and scale.numel() == 2 and scale.is_contiguous()):
             raise ValueError(f"scale: two fp32 numbers on CUDA device {device} are required")
         args = _ADAMW_ARGS(lr, beta1, beta2, eps, step, seed & 0xFFFFFFFFFFFFFFFF, 0 if scale is None else scale.data_ptr(), state.bits, TYPE_CODES[kind])
-        rc = self.lib.atomo_adamw(self._h, state._desc, struct.pack("=%dQ" % n, *map(_T.data_ptr, grads)), n, args, self._own_stream())
+        rc = self.lib.atomo_adamw(self._h, state._desc, state._pack(*map(_T.data_ptr, grads)), n, args, self._own_stream())
         _written(state.params)
         self._check(rc, "atomo_adamw")
 

@@ -481,3 +481,27 @@ def test_refused_tensors(atomo):
         api.AdamWState([p], [torch.zeros(64, device="cuda", dtype=torch.bfloat16)], [torch.zeros(64, device="cuda")])
     with pytest.raises(ValueError):
         api.AdamWState([torch.zeros(8, 8, device="cuda").t()[:4]], [torch.zeros(32, device="cuda")], [torch.zeros(32, device="cuda")])
+
+
+def test_parameters_that_were_given_other_memory(atomo):
+    """The call refuses them, and what its description names is still allocated: nothing else gets that memory meanwhile."""
+    from paper_1806_04090_b200 import api
+    n = 1 << 18
+    p, q = torch.nn.Parameter(torch.zeros(n, device="cuda")), torch.nn.Parameter(torch.zeros(77, device="cuda"))
+    state = api.AdamWState.zeros([p, q], bits=8, weight_decay=0.0)
+    grads = [torch.ones(n, device="cuda"), torch.ones(77, device="cuda")]
+    atomo.atomo_adamw(state, grads, lr=0.1, step=1)
+    first = p.detach().clone()
+    old = p.data_ptr()
+    p.data = p.data.clone()
+    with pytest.raises(ValueError, match="other memory"):
+        atomo.atomo_adamw(state, grads, lr=0.1, step=2)
+    assert torch.equal(p.detach(), first)
+    assert all(torch.empty(n, device="cuda").data_ptr() != old for _ in range(4))
+    moved = api.AdamWState([p, q], state.exp_avg, state.exp_avg_sq, state.exp_avg_scale, state.exp_avg_sq_scale, weight_decay=0.0)
+    atomo.atomo_adamw(moved, grads, lr=0.1, step=2)
+    assert bool((p < first).all())
+    # states: the memory that is described stays allocated
+    old = state.exp_avg[0].data_ptr()
+    state.exp_avg[0].data = torch.zeros(n, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    assert all(torch.empty(n, dtype=torch.uint8, device="cuda").data_ptr() != old for _ in range(4))
