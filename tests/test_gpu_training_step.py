@@ -1,5 +1,10 @@
 """GPU: a training step from the tokens to the weights as it is used: embedding, layer norm and their gradients, both workers' gradients encoded,
 the payloads averaged, norm and clipping, AdamW."""
+import dataclasses
+import os
+import re
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -125,3 +130,76 @@ def test_step_as_a_captured_graph(atomo, rows, cols, tokens, dtype, bits):
     torch.cuda.synchronize()
     for a, b in zip(eager + eager_state.exp_avg + eager_state.exp_avg_sq, params + state.exp_avg + state.exp_avg_sq):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def _readme_step():
+    """The lines of the README that show a step."""
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        blocks = re.findall(r"```python\n(.*?)```", f.read(), re.S)
+    found = [b for b in blocks if "atomo_adamw" in b]
+    assert len(found) == 1
+    return found[0]
+
+
+def test_workers_that_step_as_the_readme_says_stay_alike():
+    """Two workers, a thread each, on batches of their own: after every step their weights and states are the same bit for bit, and the vectors' gradients the
+    mean of both.  (Nothing on the GPU waits for the other worker: the threads meet on the host, between calls.)"""
+    from paper_1806_04090_b200 import api
+    code = compile(_readme_step(), "README.md", "exec")
+    steps, meet = 3, threading.Barrier(2, timeout=120)
+    slots, own, results, errors = [None, None], [None, None], [None, None], []
+
+    class Exchange:
+        def __init__(self, rank):
+            self.rank = rank
+
+        def all_gather_bytes(self, buf):
+            torch.cuda.synchronize()
+            slots[self.rank] = buf
+            meet.wait()
+            both = list(slots)
+            meet.wait()
+            return both
+
+    def worker(rank):
+        try:
+            ctx = api.Atomo(0)
+            gen = torch.Generator(device="cuda")
+            gen.manual_seed(71)
+            params = [torch.randn(ROWS, COLS, generator=gen, device="cuda") * 0.3, torch.ones(COLS, device="cuda"), torch.zeros(COLS, device="cuda")]
+            state = api.AdamWState.zeros(params, bits=8)
+            gen.manual_seed(72 + rank)
+            after = []
+            for step in range(1, steps + 1):
+                ids = torch.randint(0, ROWS, (TOKENS,), generator=gen, device="cuda")
+                dy = torch.randn(TOKENS, COLS, generator=gen, device="cuda")
+                x = ctx.atomo_embedding(params[0], ids)
+                _, mean, rstd = ctx.atomo_layer_norm(x, params[1], params[2])
+                own[rank] = ctx.atomo_layer_norm_backward(dy, x, params[1], mean, rstd)[1:]
+                names = dict(atomo=ctx, dataclasses=dataclasses, dist=Exchange(rank), table=params[0], weight=params[1], bias=params[2], ids=ids, dy=dy, state=state, rank=rank, step=step)
+                exec(code, names)
+                torch.cuda.synchronize()
+                meet.wait()
+                for got, a, b in zip((names["dweight"], names["dbias"]), *own):
+                    want = (a.double() + b.double()) / 2
+                    # a kept atom is rescaled by 1 / p, p = 1 or the next number to it; the mean's sum and quotient round once each
+                    assert bool(((got.double() - want).abs() <= 4 * ref.U32 * (a.abs() + b.abs()).double()).all())
+                meet.wait()
+                after.append([t.view(torch.uint8).clone() for t in params + state.exp_avg + state.exp_avg_sq + state.exp_avg_scale + state.exp_avg_sq_scale])
+            results[rank] = after
+            torch.cuda.synchronize()
+            ctx.close()
+        except BaseException as e:                       # noqa: B036  (told by the test's own thread)
+            errors.append(e)
+            meet.abort()
+
+    threads = [threading.Thread(target=worker, args=(r,)) for r in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    if errors:
+        raise errors[0]
+    for a, b in zip(*results):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    assert not torch.equal(results[0][0][0], results[0][-1][0])
