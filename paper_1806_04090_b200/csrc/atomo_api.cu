@@ -58,6 +58,7 @@ struct atomo_ctx {
   int64_t acc_calls = 0;
   bool profiling = false;
   bool configured = false;
+  SortRoom sort_room;                // of the embedding's gradient
   int max_sweeps = 40;
   float tol = 3e-7f;
   int eig_mode = 1;                  // 1: Cholesky factor + Jacobi on its rows; 0: Jacobi on [A | I]
@@ -414,7 +415,7 @@ int atomo_create(atomo_ctx** out, int device) {
     for (int i = 0; i < ATOMO_N_STAGES; ++i) { CK(cudaEventCreate(&ctx->ev[r][i][0])); CK(cudaEventCreate(&ctx->ev[r][i][1])); }
   int e = sp_configure();
   if (e == 0) e = ew_configure();
-  if (e == 0) e = embedding_configure(device);
+  if (e == 0) e = embedding_configure(&ctx->sort_room);
   if (e == 0) e = layer_norm_configure();
   if (e != 0) return fail_cuda(ctx, (cudaError_t)e, "cudaFuncSetAttribute(max dynamic shared memory)");
   ctx->tc_ok = sp_tc_configure() == 0;
@@ -1573,7 +1574,7 @@ int atomo_embedding_backward(atomo_ctx* ctx, const void* ids, int32_t id_bytes, 
   const int64_t need = atomo_embedding_workspace_bytes(n_ids, rows, cols);
   if (need > 0 && bad_ptr(workspace, 16)) return ATOMO_ERR_INVALID_ARG;
   if (workspace_bytes < need) return ATOMO_ERR_CAPACITY;
-  const EmbBackward a{ids, id_bytes, n_ids, grad, type, ld, rows, cols, (float)scale, padding_idx, out, ld_out, accumulate != 0, status, static_cast<uint8_t*>(workspace)};
+  const EmbBackward a{ids, id_bytes, n_ids, grad, type, ld, rows, cols, (float)scale, padding_idx, out, ld_out, accumulate != 0, status, static_cast<uint8_t*>(workspace), ctx->sort_room};
   return on_device(ctx, "embedding gradient", [&] { return launch_embedding_backward(a, (cudaStream_t)stream); });
 }
 

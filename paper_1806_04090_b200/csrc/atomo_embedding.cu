@@ -742,9 +742,6 @@ EmbLayout emb_layout(int64_t n, int64_t cols) {
   return l;
 }
 
-// clusters of 1, 2, .. 16 CTAs that the GPU holds side by side, by device
-struct SortRoom { int clusters[5]; } sort_room[64];
-
 struct SortLaunch {
   cudaLaunchAttribute attr[1];
   cudaLaunchConfig_t cfg = {};
@@ -797,7 +794,7 @@ cudaError_t direct_type(DirectArgs& a, cudaStream_t st) {
 }
 }  // namespace
 
-int embedding_configure(int device) {
+int embedding_configure(SortRoom* room) {
   cudaError_t e = cudaFuncSetAttribute(emb_sort_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortTile * 16);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(emb_sort_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortTile * 8);
   // up to 48 KB of packs in flight and 25 KB of items
@@ -813,11 +810,11 @@ int embedding_configure(int device) {
   if (e != cudaSuccess) return (int)e;
   const bool wide = cudaFuncSetAttribute(emb_sort_kernel<true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
                     cudaFuncSetAttribute(emb_sort_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
-  for (int lg = 0; lg <= 4; ++lg) {
+  for (int lg = 0; lg < kSortClusters; ++lg) {
     int clusters = 0;
     const SortLaunch l(1 << lg, kSortTile * 16, nullptr);
     if ((lg < 4 || wide) && cudaOccupancyMaxActiveClusters(&clusters, emb_sort_kernel<true>, &l.cfg) != cudaSuccess) clusters = 0;
-    sort_room[device & 63].clusters[lg] = clusters;
+    room->clusters[lg] = clusters;
   }
   cudaGetLastError();
   return 0;
@@ -846,9 +843,7 @@ int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
     return (int)(b.type == ATOMO_TYPE_F32 ? direct_type<float>(d, st) : b.type == ATOMO_TYPE_BF16 ? direct_type<__nv_bfloat16>(d, st) : direct_type<__half>(d, st));
   }
   const EmbLayout l = emb_layout(b.n, b.cols);
-  int device = 0;
-  cudaError_t e = cudaGetDevice(&device);
-  if (e != cudaSuccess) return (int)e;
+  cudaError_t e = cudaSuccess;
   SortArgs s{};
   s.ids = Ids{b.ids, b.id_bytes == 8}; s.n = b.n; s.rows = b.rows; s.padding = b.padding; s.status = b.status;
   for (int i = 0; i < 2; ++i) s.items[i] = reinterpret_cast<uint64_t*>(b.ws + l.items[i]);
@@ -857,9 +852,8 @@ int launch_embedding_backward(const EmbBackward& b, cudaStream_t st) {
   while ((b.rows >> bits) != 0) ++bits;                          // ids as sort keys are 0 .. rows
   s.passes = (bits + 7) / 8; s.bits = (bits + s.passes - 1) / s.passes;
   // a token per thread up to the cluster's size
-  const SortRoom& room = sort_room[device & 63];
   int lg = 0;
-  while (lg < 4 && ((int64_t)kSortThreads << lg) < b.n && room.clusters[lg + 1] > 0) ++lg;
+  while (lg + 1 < kSortClusters && ((int64_t)kSortThreads << lg) < b.n && b.room.clusters[lg + 1] > 0) ++lg;
   const int ctas = 1 << lg;
   s.ctas = (uint32_t)ctas;
   s.segment = (b.n + ctas - 1) / ctas;

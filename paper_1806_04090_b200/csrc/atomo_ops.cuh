@@ -86,6 +86,8 @@ int launch_adamw(const atomo_adamw_tensor* tensors, const void* const* grads, in
 
 // ---- embedding (atomo_embedding.cu) ---------------------------------------------------------------
 constexpr int kEmbChunk = 32;           // sorted tokens that are summed by one group of threads
+constexpr int kSortClusters = 5;        // clusters of 1, 2, .. 16 CTAs
+struct SortRoom { int clusters[kSortClusters] = {}; };           // of each size, how many the GPU holds side by side
 struct EmbLookup {
   const void* table; int type; int64_t rows, cols, ld;
   const void* ids; int id_bytes; int64_t n;
@@ -97,8 +99,9 @@ struct EmbBackward {
   float scale; int64_t padding;         // id whose tokens are left out, or -1
   float* out; int64_t ld_out; int accumulate; int32_t* status;
   uint8_t* ws;
+  SortRoom room;
 };
-int embedding_configure(int device);                                             // shared memory, cluster size; cudaError_t
+int embedding_configure(SortRoom* room);                                         // shared memory, cluster sizes of the current device; cudaError_t
 int launch_embedding(const EmbLookup& a, cudaStream_t st);                       // cudaError_t
 uint64_t embedding_workspace(int64_t n, int64_t cols);
 int launch_embedding_backward(const EmbBackward& a, cudaStream_t st);            // cudaError_t
