@@ -258,3 +258,55 @@ def test_refused_tensors(atomo):
         atomo.atomo_embedding_backward(ids, grad, 10, padding_idx=10)
     with pytest.raises(api.AtomoError):
         atomo.atomo_embedding(table, ids, scale=math.inf)
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("kind", ["same", "ascending", "few", "random"])
+@pytest.mark.parametrize("n", [1000, 4096, 9001, 66000, 150001])
+def test_gradient_of_whole_numbers(atomo, kind, n, dtype):
+    """Sums of whole numbers below 2^24 are exact in fp32 in whatever order: not one token may be lost or taken twice, however long its run."""
+    gen = _gen(12)
+    for rows, cols in ((257, 20), (40, 33), (3, 260)):
+        ids = _ids(kind, n, rows, gen)
+        grad = torch.randint(-8, 9, (n, cols), generator=gen, device="cuda")
+        want = torch.zeros(rows, cols, dtype=torch.int64, device="cuda").index_add_(0, ids, grad)
+        assert int(want.abs().max()) < 1 << 24
+        got = atomo.atomo_embedding_backward(ids, grad.to(dtype), rows, scale=0.5)
+        assert torch.equal(got, want.float() * 0.5)
+        atomo.atomo_embedding_backward(ids, grad.to(dtype), rows, scale=0.5, out=got, accumulate=True)
+        assert torch.equal(got, want.float())
+
+
+@pytest.mark.parametrize("dtype,cols", [(torch.float32, 260), (torch.float32, 384), (torch.float32, 257), (torch.float32, 383), (torch.bfloat16, 528), (torch.bfloat16, 768),
+                                        (torch.float16, 522), (torch.float16, 766), (torch.bfloat16, 261), (torch.float16, 383)])
+def test_rows_of_65_to_96_packs(atomo, dtype, cols):
+    """Rows that a block of 96 x 2 threads takes, in all three widths of a pack."""
+    gen = _gen(13)
+    rows, n = 61, 6001
+    ids = _ids("few", n, rows, gen)
+    table = torch.randn(rows, cols, generator=gen, device="cuda").to(dtype)
+    assert torch.equal(atomo.atomo_embedding(table, ids), table[ids])
+    grad = torch.randn(n, cols, generator=gen, device="cuda").to(dtype)
+    want, off = _want(ids, grad, rows, 1.0)
+    ref.near(atomo.atomo_embedding_backward(ids, grad, rows), want, off)
+    whole = torch.randint(-8, 9, (n, cols), generator=gen, device="cuda")
+    assert torch.equal(atomo.atomo_embedding_backward(ids, whole.to(dtype), rows), torch.zeros(rows, cols, device="cuda").index_add_(0, ids, whole.float()))
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("cols,ld,first", [(33, 34, 1), (33, 35, 0), (257, 259, 2), (300, 304, 1), (300, 304, 4), (64, 72, 8), (1, 3, 1), (513, 515, 1)])
+def test_gradient_of_long_lists_in_strided_and_shifted_rows(atomo, dtype, cols, ld, first):
+    """Gradient rows that start anywhere and lie apart, of lists that are sorted by a kernel of their own; the buffer ends with the last row's last value."""
+    gen = _gen(14)
+    rows, n = 50, 5003
+    ids = _ids("few", n, rows, gen)
+    buffer = torch.randint(-8, 9, ((n - 1) * ld + first + cols,), generator=gen, device="cuda").to(dtype)
+    grad = buffer.as_strided((n, cols), (ld, 1), first)
+    want = torch.zeros(rows, cols, device="cuda").index_add_(0, ids, grad.float())
+    assert torch.equal(atomo.atomo_embedding_backward(ids, grad, rows), want)
+    room = torch.full((rows * (ld + 1) + 8,), 7.0, device="cuda")
+    out = room.as_strided((rows, cols), (ld + 1, 1), 3)
+    atomo.atomo_embedding_backward(ids.int(), grad, rows, out=out)
+    assert torch.equal(out, want)
+    out.fill_(7.0)
+    assert bool((room == 7.0).all())

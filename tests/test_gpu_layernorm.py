@@ -272,3 +272,16 @@ def test_rows_without_variance_and_no_eps(atomo, rows, cols, dtype):
     others = torch.arange(rows, device="cuda") != rows // 2
     for a, b in zip((y, mean, rstd), want):
         assert torch.equal(a[others], b[others])
+
+
+@pytest.mark.parametrize("dtype", ref.TYPES)
+@pytest.mark.parametrize("rows,cols", [(1, 96), (31, 1023), (64, 4096), (333, 770), (9, 8192), (40000, 48), (40000, 260), (5000, 1023), (700, 8200), (33, 16385)])
+def test_sums_over_rows_of_whole_numbers(atomo, rows, cols, dtype):
+    """With a mean of 0 and an rstd of 1, dweight and dbias are sums of whole numbers below 2^24, exact in fp32 in whatever order: not one row may be lost."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(42)
+    x, dy = (torch.randint(-8, 9, (rows, cols), generator=gen, device="cuda") for _ in range(2))
+    zeros, ones = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    _, dweight, dbias = atomo.atomo_layer_norm_backward(dy.to(dtype), x.to(dtype), torch.ones(cols, device="cuda"), zeros, ones)
+    assert int((dy * x).sum(0).abs().max()) < 1 << 24
+    assert torch.equal(dweight, (dy * x).sum(0).float()) and torch.equal(dbias, dy.sum(0).float())
