@@ -260,6 +260,7 @@ int atomo_decode_spectral_static(int device, const void* payload /*DEVICE*/, con
  *   - Values are fp32, bf16 or fp16 (atomo_type); arithmetic, sums and statistics are in fp32 or fp64, and a result is rounded to
  *     its type once, to the nearest value.  Pointers need the alignment of their type alone; 16-byte aligned
  *     rows and tensors are moved faster.
+ *   - Numbers given by the host (scale, lr, eps) enter the arithmetic as fp32: what is beyond its range is refused.
  *   - No call allocates or waits on the host: what a call needs beside its operands is a workspace of the caller
  *     (atomo_*_workspace_bytes, host only; contents need not be kept), so that calls on several streams, and CUDA graphs that hold
  *     them, share nothing.  A captured call keeps the host values it was captured with (learning rate, step, seed).

@@ -367,6 +367,8 @@ struct DeviceScope {                 // the context's device for the call, the c
   }
   ~DeviceScope() { if (changed) cudaSetDevice(before); }
 };
+// host numbers reach the kernels as fp32
+bool bad_fp32(double x) { return !std::isfinite((float)x); }
 bool bad_type(int type) { return type < ATOMO_TYPE_F32 || type > ATOMO_TYPE_F16; }
 bool off_type(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
 // null, or not aligned to its elements
@@ -1531,7 +1533,7 @@ int atomo_grad_norm(atomo_ctx* ctx, const atomo_tensor* grads, int32_t n_tensors
 int atomo_adamw(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, const void* const* grads, int32_t n_tensors, const atomo_adamw_args* args, void* stream) {
   if (!ctx || !tensors || !grads || n_tensors <= 0 || !args) return ATOMO_ERR_INVALID_ARG;
   const atomo_adamw_args& a = *args;
-  if (!(a.lr >= 0.0) || !std::isfinite(a.lr) || !(a.eps >= 0.0) || !std::isfinite(a.eps) || !(a.beta1 >= 0.0 && a.beta1 < 1.0) || !(a.beta2 >= 0.0 && a.beta2 < 1.0) || a.step < 1)
+  if (!(a.lr >= 0.0) || bad_fp32(a.lr) || !(a.eps >= 0.0) || bad_fp32(a.eps) || !(a.beta1 >= 0.0 && a.beta1 < 1.0) || !(a.beta2 >= 0.0 && a.beta2 < 1.0) || a.step < 1)
     return ATOMO_ERR_INVALID_ARG;
   if ((a.state_bits != 32 && a.state_bits != 8) || bad_type(a.grad_type) || off_type(a.scale, 4)) return ATOMO_ERR_INVALID_ARG;
   const bool small = a.state_bits == 8;
@@ -1547,6 +1549,7 @@ int atomo_adamw(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, const void* c
   h.lr = (float)a.lr; h.eps = (float)a.eps;
   h.step_size = (float)(a.lr / (1.0 - std::pow(a.beta1, (double)a.step)));
   h.inv_root_bias2 = (float)(1.0 / std::sqrt(1.0 - std::pow(a.beta2, (double)a.step)));
+  if (!std::isfinite(h.step_size)) return ATOMO_ERR_INVALID_ARG;
   h.scale = a.scale; h.step = (uint32_t)a.step; h.grad_type = a.grad_type;
   h.key = philox_round_keys(PhiloxKey{(uint32_t)a.seed, (uint32_t)(a.seed >> 32)});
   return on_device(ctx, "adamw", [&] { return launch_adamw(tensors, grads, n_tensors, a.state_bits, h, (cudaStream_t)stream); });
@@ -1555,7 +1558,7 @@ int atomo_adamw(atomo_ctx* ctx, const atomo_adamw_tensor* tensors, const void* c
 int atomo_embedding(atomo_ctx* ctx, const void* table, int32_t type, int64_t rows, int64_t cols, int64_t ld, const void* ids, int32_t id_bytes, int64_t n_ids,
                     double scale, void* out, int64_t ld_out, int32_t* status, void* stream) {
   if (!ctx || bad_type(type) || rows <= 0 || bad_shape(rows, cols, ld) || bad_shape(n_ids, cols, ld_out) || (id_bytes != 4 && id_bytes != 8)) return ATOMO_ERR_INVALID_ARG;
-  if (!std::isfinite(scale) || bad_ptr(table, type_bytes(type)) || off_type(status, 4)) return ATOMO_ERR_INVALID_ARG;
+  if (bad_fp32(scale) || bad_ptr(table, type_bytes(type)) || off_type(status, 4)) return ATOMO_ERR_INVALID_ARG;
   if (n_ids > 0 && (bad_ptr(ids, id_bytes) || bad_ptr(out, type_bytes(type)))) return ATOMO_ERR_INVALID_ARG;
   const EmbLookup a{table, type, rows, cols, ld, ids, id_bytes, n_ids, (float)scale, out, ld_out, status};
   return on_device(ctx, "embedding", [&] { return launch_embedding(a, (cudaStream_t)stream); });
@@ -1569,7 +1572,7 @@ int64_t atomo_embedding_workspace_bytes(int64_t n_ids, int64_t rows, int64_t col
 int atomo_embedding_backward(atomo_ctx* ctx, const void* ids, int32_t id_bytes, int64_t n_ids, const void* grad, int32_t type, int64_t ld, int64_t rows, int64_t cols,
                              double scale, int64_t padding_idx, float* out, int64_t ld_out, int32_t accumulate, int32_t* status, void* workspace, int64_t workspace_bytes, void* stream) {
   if (!ctx || bad_type(type) || rows <= 0 || bad_shape(rows, cols, ld_out) || bad_shape(n_ids, cols, ld) || (id_bytes != 4 && id_bytes != 8)) return ATOMO_ERR_INVALID_ARG;
-  if (!std::isfinite(scale) || bad_ptr(out, 4) || off_type(status, 4) || padding_idx < -1 || padding_idx >= rows) return ATOMO_ERR_INVALID_ARG;
+  if (bad_fp32(scale) || bad_ptr(out, 4) || off_type(status, 4) || padding_idx < -1 || padding_idx >= rows) return ATOMO_ERR_INVALID_ARG;
   if (n_ids > 0 && (bad_ptr(ids, id_bytes) || bad_ptr(grad, type_bytes(type)))) return ATOMO_ERR_INVALID_ARG;
   const int64_t need = atomo_embedding_workspace_bytes(n_ids, rows, cols);
   if (need > 0 && bad_ptr(workspace, 16)) return ATOMO_ERR_INVALID_ARG;
@@ -1580,7 +1583,7 @@ int atomo_embedding_backward(atomo_ctx* ctx, const void* ids, int32_t id_bytes, 
 
 int atomo_layer_norm(atomo_ctx* ctx, const void* x, int32_t type, int64_t rows, int64_t cols, int64_t ld, const void* weight, const void* bias, int32_t weight_type,
                      double eps, void* y, int64_t ld_y, float* mean, float* rstd, void* stream) {
-  if (!ctx || bad_type(type) || bad_type(weight_type) || rows > kNormRows || bad_shape(rows, cols, ld) || bad_shape(rows, cols, ld_y) || !(eps >= 0.0) || !std::isfinite(eps)) return ATOMO_ERR_INVALID_ARG;
+  if (!ctx || bad_type(type) || bad_type(weight_type) || rows > kNormRows || bad_shape(rows, cols, ld) || bad_shape(rows, cols, ld_y) || !(eps >= 0.0) || bad_fp32(eps)) return ATOMO_ERR_INVALID_ARG;
   if (off_type(weight, type_bytes(weight_type)) || off_type(bias, type_bytes(weight_type))) return ATOMO_ERR_INVALID_ARG;
   if (rows > 0 && (bad_ptr(x, type_bytes(type)) || bad_ptr(y, type_bytes(type)) || bad_ptr(mean, 4) || bad_ptr(rstd, 4))) return ATOMO_ERR_INVALID_ARG;
   const NormForward a{x, type, rows, cols, ld, weight, bias, weight_type, (float)eps, y, ld_y, mean, rstd};

@@ -140,3 +140,15 @@ def test_rows_of_a_tensor():
             api._rows(bad, cols, "x")
     with pytest.raises(ValueError):
         api._rows(x, 5, "x")
+
+
+def test_host_numbers_beyond_fp32(ctx):
+    """Finite in 64 bits, Inf in the kernels' arithmetic."""
+    lib, h = ctx
+    step = lambda lr, eps, step=1, b1=0.9: lib.atomo_adamw(h, (api._AdamWTensor * 1)((GOOD, GOOD, GOOD, None, None, None, 0, 0.0, 0)), (ctypes.c_void_p * 1)(GOOD), 1,  # noqa: E731
+                                                           ctypes.byref(api._AdamWArgs(lr, b1, 0.999, eps, step, 0, None, 32, 0)), None)
+    assert step(1e39, 1e-8) == step(1e-3, 1e39) == step(1e38, 1e-8) == INVALID          # (1e38 / (1 - 0.9) is beyond it too)
+    for s in (1e39, -1e300):
+        assert lib.atomo_embedding(h, GOOD, 0, 8, 4, 4, GOOD, 8, 3, s, GOOD, 4, None, None) == INVALID
+        assert lib.atomo_embedding_backward(h, GOOD, 8, 3, GOOD, 0, 4, 8, 4, s, -1, GOOD, 4, 0, None, GOOD, 1 << 30, None) == INVALID
+    assert lib.atomo_layer_norm(h, GOOD, 0, 3, 4, 4, GOOD, GOOD, 0, 1e39, GOOD, 4, GOOD, GOOD, None) == INVALID
