@@ -271,8 +271,8 @@ typedef struct { const void* data; /* DEVICE */ int64_t n; int32_t type; /* atom
 
 /* --- gradient norm -----------------------------------------------------------------------------
  * out[0] = sqrt(sum of the squares of all elements of all tensors), out[1] = min(1, max_norm / (out[0] + 1e-6)): the norm and the
- * factor that clips the gradients to it.  max_norm > 0; INFINITY asks for the norm alone (factor 1).  The sum neither
- * overflows nor underflows: out[0] is the norm rounded to fp32.  Where an element is NaN or Inf the norm is not finite and
+ * factor that clips the gradients to it.  max_norm > 0; INFINITY asks for the norm alone (factor 1).  Squares are added in
+ * fp32 over up to 32 values and in fp64 from there on, so that the sum neither overflows nor underflows and out[0] is the norm to 17 half-units of fp32.  Where an element is NaN or Inf the norm is not finite and
  * the factor is NaN.  Tensors may be empty; at most 2^20 of them, of 2^40 values in all.  workspace: atomo_grad_norm_workspace_bytes (0, and NULL will do, where little is
  * to be read; -1 on bad arguments).                                                                                              */
 int64_t atomo_grad_norm_workspace_bytes(const atomo_tensor* grads /*HOST array*/, int32_t n_tensors);

@@ -829,7 +829,8 @@ int launch_embedding(const EmbLookup& a, cudaStream_t st) {
 
 // One launch, or four.  Kernels alone, us, one | four (tokens x rows x columns, fp32): 256 x 21294 x 38 6 | 19, 1000 x 5000 x 64 6 | 24, 1000 x 32000 x 1024 27 | 34,
 // 2000 x 32000 x 2048 56 | 57, 3000 x 32000 x 1024 36 | 36, 4000 x 16000 x 1024 28 | 27, 4000 x 50000 x 512 32 | 30, 4001 x 10007 x 515 22 | 25, 4000 x 32000 x 2048
-// 66 | 59 (bf16 alike): a frequent id's tokens wait for one CTA, the longer the more there are and the wider they are.
+// 66 | 59 (bf16 alike): a frequent id's tokens wait for one CTA, the longer the more there are and the wider they are.  The rule knows neither the rows, which move the
+// crossing (4000 x 50000 x 512 takes the one launch, 2 us slower), nor the ids' distribution (these are Zipf's).  One launch spares the host 13 us a call.
 static bool one_launch(int64_t n, int64_t cols) { return n <= 2048 || (n <= kDirectMost && n * cols <= 5 << 19); }
 uint64_t embedding_workspace(int64_t n, int64_t cols) { return one_launch(n, cols) ? 0 : emb_layout(n, cols).bytes; }
 

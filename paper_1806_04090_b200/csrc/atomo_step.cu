@@ -12,7 +12,8 @@ namespace {
 // =================================== norm ========================================================
 // sqrt(sum g^2).  Squares are summed in fp32 over the 16 or 32 values that a thread has in registers and in fp64 from there on.  Where
 // such a sum is not well inside the range of fp32 (values around 1e19 or 1e-14 and beyond, all of them zero, NaN or Inf) it is
-// formed again in fp64 from the registers: the norm neither overflows nor loses small gradients, and rounds to fp32 once, at the end.
+// formed again in fp64 from the registers: the norm neither overflows nor loses small gradients.  (It is right to 17 half-units: up to 32 fused sums
+// in fp32, halved by the root, and the result's own rounding.)
 // 133M fp32 values (534 MB): 83 us, 6.4 TB/s, what a copy reaches.  Up to 1 MB goes through one cluster of up to eight CTAs: one launch, 4 us.
 constexpr int kNormThreads = 256, kNormLoads = 4;
 constexpr int kNormChunk = kNormThreads * kNormLoads * 16;     // bytes per step of a CTA
@@ -588,7 +589,7 @@ __device__ __forceinline__ void adam_inside(const AdamTensor& t, const AdamHyper
 
 // Chunks of 2048 elements and five CTAs per SM, us (8-bit states, 25.6M elements | fp32 states, 11M | fp32 states and master copy, 133M): 74 | 51 | 550;
 // of 4096 and three per SM: 78 | 53 | 553; of 4096 and four: 90 | 53 | 562; of 2048 and six: 83 | 51 | 553.  The update by pairs took the instructions per
-// element with 8-bit states from 65 to 53 (issue slots 62 % busy).  Memory bounds all three: 413, 308 and 3738 MB, 5.6, 6.0 and 6.8 TB/s.
+// element with 8-bit states from 65 to 53, its moments rounded operation by operation to 54 (issue slots 62 % busy).  Memory bounds all three: 413, 308 and 3738 MB, 5.6, 6.0 and 6.8 TB/s.
 template <int N, int BITS>
 __global__ void __launch_bounds__(kAdamThreads, 5) adamw_kernel(const __grid_constant__ AdamBatch<N> B) {
   int lo = 0, hi = B.n - 1;                                      // the last tensor that starts at or before this chunk
