@@ -553,6 +553,7 @@ __global__ void __launch_bounds__(kLongThreads) ln_backward_long_kernel(const T*
     store_pack<T, VEC>(dx + row * ld_dx + c, d);
   }
 }
+constexpr int kLongRows = 32;                                    // of a partial sum, at least
 // partial sums of dw and db: a CTA takes 256 VEC columns of every gridDim.y-th row
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) ln_columns_kernel(const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ x, int64_t ld_x, int64_t rows, int cols,
@@ -691,7 +692,7 @@ cudaError_t backward_type(const NormBackward& a, cudaStream_t st) {
   if (a.rows == 0) return backward_join(a, 0, st);
   const int bytes = std::min({pack_bytes(a.x, a.ld_x, a.cols, sizeof(T)), pack_bytes(a.dy, a.ld_dy, a.cols, sizeof(T)), pack_bytes(a.dx, a.ld_dx, a.cols, sizeof(T))});
   if (a.cols > kNormCols) {
-    const int split = back_ctas(a.rows, 32);                     // first, since dx may lie where dy or x does
+    const int split = back_ctas(a.rows, kLongRows);              // first, since dx may lie where dy or x does
     auto launch = [&](auto columns, auto kernel, int vec) {
       columns<<<dim3((unsigned)((a.cols + 256 * vec - 1) / (256 * vec)), split), 256, 0, st>>>((const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, a.rows, (int)a.cols, a.mean, a.rstd, a.ws);
       kernel<<<(unsigned)a.rows, kLongThreads, 0, st>>>((const T*)a.dy, a.ld_dy, (const T*)a.x, a.ld_x, (int)a.cols, Weight{a.weight, a.weight_type}, a.mean, a.rstd, (T*)a.dx, a.ld_dx);
@@ -733,7 +734,8 @@ int launch_layer_norm(const NormForward& a, cudaStream_t st) {
 
 uint64_t layer_norm_workspace(int64_t rows, int64_t cols) {
   if (one_launch(rows, cols)) return 0;
-  return (uint64_t)std::min<int64_t>(rows, kBackCtas) * 2 * cols * 4;
+  const int parts = cols > kNormCols ? back_ctas(rows, kLongRows) : (int)std::min<int64_t>(rows, kBackCtas);
+  return (uint64_t)parts * 2 * cols * 4;
 }
 
 int launch_layer_norm_backward(const NormBackward& a, cudaStream_t st) {

@@ -152,3 +152,12 @@ def test_host_numbers_beyond_fp32(ctx):
         assert lib.atomo_embedding(h, GOOD, 0, 8, 4, 4, GOOD, 8, 3, s, GOOD, 4, None, None) == INVALID
         assert lib.atomo_embedding_backward(h, GOOD, 8, 3, GOOD, 0, 4, 8, 4, s, -1, GOOD, 4, 0, None, GOOD, 1 << 30, None) == INVALID
     assert lib.atomo_layer_norm(h, GOOD, 0, 3, 4, 4, GOOD, GOOD, 0, 1e39, GOOD, 4, GOOD, GOOD, None) == INVALID
+
+
+def test_layer_norm_workspace_of_long_rows(ctx):
+    """Of rows that several CTAs read again, a partial sum of the weight's and the bias's gradient for each 32 rows: never a multiple of the operands."""
+    lib, _ = ctx
+    size = lib.atomo_layer_norm_workspace_bytes
+    for rows, cols in ((1, 8193), (32, 1 << 20), (592, 1 << 22), (100000, 16384)):
+        assert size(rows, cols) == min(-(-rows // 32), 592) * 2 * cols * 4
+        assert size(rows, cols) <= max(rows // 16, 2) * cols * 4 + 8 * cols
