@@ -765,7 +765,7 @@ class Atomo:
     def atomo_embedding(self, table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
                         status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
         """scale * table[ids], of shape ids.shape + (cols,).  An id outside the table gives a row of zeros and raises `status` (one int32, set to
-        zero by the caller) to ATOMO_ERR_INVALID_ARG."""
+        zero by the caller) to ATOMO_ERR_INVALID_ARG.  out must not overlap the table."""
         if stream is not None:
             return self._on(stream, self.atomo_embedding, table, ids, scale, out, status)
         kind = self._operand(table, "table").dtype
